@@ -28,6 +28,10 @@
  *   fupr_conv_maxpool_fused             Table II's ImageNet stem (7 x 7 convolution, stride 2, then
  *                        3 x 3 max pool, stride 2) in one kernel
  *   fupr_model_*, fupr_forward          a whole network (Table II) on one stream
+ *   fupr_linear_fused                   a layer of a feed-forward network on rows of tokens: matrix product with
+ *                        bias, activation, gate and residual in its epilogue
+ *   fupr_moe_route, fupr_expert_linear_fused, fupr_moe_combine   a mixture of experts, each with its own number
+ *                        of rows and, after filter pruning, its own widths
  *
  * Conventions
  *   - Host calls (fold, select, prune, pack, model create) take HOST pointers.
@@ -370,6 +374,130 @@ fupr_status fupr_conv_conv1x1_fused(const fupr_conv_shape* shape1, const fupr_te
                                     const fupr_tensor* y, const fupr_conv_shape* shape2,
                                     const void* packed2, uint32_t flags2, const fupr_tensor* h,
                                     void* stream);
+
+/* ---------------------------------------------------- feed-forward layers -- */
+
+/*
+ * A matrix in device memory: rows x cols elements of type dt, element (r, c) at ptr[r * stride + c].  stride >= cols
+ * is a multiple of 8 for 16-bit types and of 4 for fp32, ptr is 16-byte aligned, and the memory holds rows * stride
+ * elements.  What lies in the lanes cols .. stride - 1 is read by nobody's result (it may be anything, NaN
+ * included) and is not written.  rows may be 0; then nothing is launched.
+ */
+typedef struct {
+  int32_t rows, cols;
+  int64_t stride;
+  fupr_dtype dt;
+  void* ptr; /* [dev] */
+} fupr_matrix;
+
+/* a(v):  v;  max(v, 0);  v / (1 + e^-v);  v Phi(v);  v / (1 + e^-2u), u = sqrt(2/pi) (v + 0.044715 v^3).
+ * A NaN stays a NaN under each of them. */
+enum {
+  FUPR_ACT_NONE = 0,
+  FUPR_ACT_RELU = 1,
+  FUPR_ACT_SILU = 2,
+  FUPR_ACT_GELU = 3,
+  FUPR_ACT_GELU_TANH = 4
+};
+
+/*
+ * A linear layer: N filters of K weights, row n of w at w + n * w_stride elements (alignment as for fupr_matrix;
+ * the model's own layout, nothing is packed).  With w_up the layer is gated: w is the gate, w_up (same sizes and
+ * stride) what it multiplies.
+ */
+typedef struct {
+  int32_t N, K;
+  fupr_dtype dt;
+  int32_t act;            /* FUPR_ACT_* */
+  int64_t w_stride;
+  const void* w;          /* [dev] N x K */
+  const void* w_up;       /* [dev] N x K, or NULL */
+  const float* bias;      /* [dev] N, or NULL */
+  const float* bias_up;   /* [dev] N, or NULL; only with w_up */
+} fupr_linear;
+
+/*
+ * y = a(x w^T + bias) (* (x w_up^T + bias_up)) (+ res): products accumulated in fp32, the epilogue in fp32, one
+ * rounding to y's type.  x: rows x K of type op->dt; y, res: rows x N of one type, op->dt or FUPR_F32.  res may be
+ * NULL.  y must not overlap x or the weights, and may overlap res only as the same matrix (same ptr, stride, type).
+ * The sum over K is taken in an order that depends on the sizes only: the same call gives the same bits.
+ *
+ * workspace is [dev], 256-byte aligned, at least fupr_linear_workspace_bytes() bytes for at least as many rows (0
+ * bytes: may be NULL).  It holds zeros when it is first used and is left holding what the next call needs, whatever
+ * that call's sizes; calls that share one are ordered by the caller.  Nothing else passes from call to call in it.
+ * Asynchronous and capturable.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, ARG (unknown activation, bias_up without w_up, overlap), WORKSPACE, LIMIT, LAUNCH.
+ */
+size_t fupr_linear_workspace_bytes(const fupr_linear* op, int32_t rows); /* 0 for an invalid op too */
+fupr_status fupr_linear_fused(const fupr_linear* op, const fupr_matrix* x, const fupr_matrix* res, const fupr_matrix* y,
+                              void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The linear layers of E experts of one shape: `one` describes expert 0, expert e's weights lie e * w_expert_stride
+ * elements further (w and w_up alike; a multiple of 8, fp32: 4), its biases e * N floats further.  n_len, k_len: how
+ * many of the N filters and of the K inputs of each expert are left (filter pruning takes them at the end:
+ * fupr_prune moves the kept ones to the front); NULL: all.  Values outside 0 .. N or 0 .. K are clamped.
+ */
+typedef struct {
+  fupr_linear one;
+  int32_t E;
+  int64_t w_expert_stride;
+  const int32_t* n_len;   /* [dev] E, or NULL */
+  const int32_t* k_len;   /* [dev] E, or NULL */
+} fupr_expert_linear;
+
+/*
+ * fupr_linear_fused of every expert on its own rows: rows offsets[e] .. offsets[e + 1] - 1 of y are expert e's result
+ * for the rows src[r] of x (src NULL: row r of x).  Columns n_len[e] .. N - 1 of y become 0.  Rows below offsets[0]
+ * and from offsets[E] on are left as they are.  offsets [dev]: E + 1 int32, ascending, within 0 .. y->rows; src [dev]:
+ * y->rows int32, within 0 .. x->rows - 1 at the rows in use (what fupr_moe_route writes).  With other content the
+ * values of y are unspecified, but no access leaves x, y or the weights.  No host read of the counts: the
+ * launch covers any distribution of y->rows rows over the experts.  workspace as in fupr_linear_fused.
+ * Errors: those of fupr_linear_fused.
+ */
+size_t fupr_expert_linear_workspace_bytes(const fupr_expert_linear* op, int32_t rows);
+fupr_status fupr_expert_linear_fused(const fupr_expert_linear* op, const fupr_matrix* x, const int32_t* offsets,
+                                     const int32_t* src, const fupr_matrix* y, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/*
+ * Which experts a token goes to.  score(t, e): softmax of the token's logits over the experts that exist, or the
+ * sigmoid of each.  Chosen are the top_k experts of largest logit - with select_bias, of largest score + bias
+ * (compared in fp64) -, the lower index first among equals.  An expert does not exist for a token if keep is 0 or its logit
+ * (or its biased score) is -inf; a NaN ranks above every number.  weight = scale * score, with renormalise divided
+ * by the sum of the chosen scores.
+ */
+enum { FUPR_SCORE_SOFTMAX = 0, FUPR_SCORE_SIGMOID = 1 };
+typedef struct {
+  int32_t E, top_k;            /* 1 <= top_k <= min(E, 16), E <= 1024 */
+  int32_t score;               /* FUPR_SCORE_* */
+  int32_t renormalise;         /* 0 or 1 */
+  float scale;
+  const uint8_t* keep;         /* [dev] E, 0: the expert was pruned away; or NULL */
+  const float* select_bias;    /* [dev] E, or NULL */
+} fupr_router;
+
+/*
+ * ids, weights [dev] T x top_k: the chosen experts of each token, best first; -1 and weight 0 where fewer exist.
+ * offsets [dev] E + 1, src, pos [dev] T * top_k: the rows of an expert's products, ordered by expert and then by
+ * token.  Row r is token src[r]'s, slot (t, j) has row pos[t * top_k + j]; src is -1 from offsets[E] on, pos -1 at slots
+ * without an expert.  logits: T x E, any type.  workspace [dev] as fupr_moe_route_workspace_bytes() says, 256-byte
+ * aligned; nothing is expected of what it holds.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, ARG, WORKSPACE, LIMIT, LAUNCH.
+ */
+size_t fupr_moe_route_workspace_bytes(const fupr_router* router, int32_t tokens);
+fupr_status fupr_moe_route(const fupr_router* router, const fupr_matrix* logits, int32_t* ids, float* weights,
+                           int32_t* offsets, int32_t* src, int32_t* pos, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/*
+ * out[t] = (res[t] +) sum_j weights[t, j] * y[pos[t, j]], j ascending, in fp32, rounded once; a slot whose pos is not
+ * a row of y adds nothing.  weights, pos [dev] T x top_k; y, res, out share columns and type; out may be res itself and
+ * otherwise overlaps nothing.
+ * Errors: NULL, SHAPE, DTYPE, ALIGN, ARG, LIMIT, LAUNCH.
+ */
+fupr_status fupr_moe_combine(const fupr_matrix* y, const int32_t* pos, const float* weights, int32_t top_k,
+                             const fupr_matrix* res, const fupr_matrix* out, void* stream);
 
 /* ----------------------------------------------------------------- model -- */
 

@@ -35,6 +35,8 @@ CAT_ALIGN = 64   # FUPR_CAT_ALIGN
 OP_CONV, OP_MAXPOOL, OP_AVGPOOL = 0, 1, 2
 SHORTCUT_IDENTITY, SHORTCUT_SUBSAMPLE_PAD, SHORTCUT_PROJECTION = 0, 1, 2
 SCHEDULE_AUTO, SCHEDULE_PER_LAYER = 0, 1
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+SCORES = {"softmax": 0, "sigmoid": 1}
 DTYPES = {"f32": F32, "bf16": BF16, "f16": F16}
 
 
@@ -92,11 +94,37 @@ class OpStats(C.Structure):
                 ("kernel", C.c_char_p)]
 
 
+class Matrix(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("stride", C.c_int64), ("dt", C.c_int),
+                ("ptr", C.c_void_p)]
+
+
+_MATRIX = struct.Struct("@iiqiP").pack   # the fields of Matrix as C lays them out
+assert len(_MATRIX(0, 0, 0, 0, 0)) == C.sizeof(Matrix)
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [("N", C.c_int32), ("K", C.c_int32), ("dt", C.c_int), ("act", C.c_int32), ("w_stride", C.c_int64),
+                ("w", C.c_void_p), ("w_up", C.c_void_p), ("bias", C.c_void_p), ("bias_up", C.c_void_p)]
+
+
+class ExpertLinearDesc(C.Structure):
+    _fields_ = [("one", LinearDesc), ("E", C.c_int32), ("w_expert_stride", C.c_int64), ("n_len", C.c_void_p),
+                ("k_len", C.c_void_p)]
+
+
+class RouterDesc(C.Structure):
+    _fields_ = [("E", C.c_int32), ("top_k", C.c_int32), ("score", C.c_int32), ("renormalise", C.c_int32),
+                ("scale", C.c_float), ("keep", C.c_void_p), ("select_bias", C.c_void_p)]
+
+
 _F = C.POINTER(C.c_float)
 _U8 = C.POINTER(C.c_uint8)
 _I32 = C.POINTER(C.c_int32)
 _SH = C.POINTER(ConvShape)
 _T = C.POINTER(Tensor)
+_M = C.POINTER(Matrix)
+_V = C.c_void_p
 
 # Every symbol include/fupr.h declares, with its C signature.
 SIGNATURES = {
@@ -147,6 +175,13 @@ SIGNATURES = {
     "fupr_graph_launch": (C.c_int32, [C.c_void_p, C.c_void_p]),
     "fupr_graph_destroy": (None, [C.c_void_p]),
     "fupr_tuning_set": (C.c_int32, [C.c_char_p, C.c_char_p]),
+    "fupr_linear_workspace_bytes": (C.c_size_t, [C.POINTER(LinearDesc), C.c_int32]),
+    "fupr_linear_fused": (C.c_int32, [C.POINTER(LinearDesc), _M, _M, _M, _V, C.c_size_t, _V]),
+    "fupr_expert_linear_workspace_bytes": (C.c_size_t, [C.POINTER(ExpertLinearDesc), C.c_int32]),
+    "fupr_expert_linear_fused": (C.c_int32, [C.POINTER(ExpertLinearDesc), _M, _V, _V, _M, _V, C.c_size_t, _V]),
+    "fupr_moe_route_workspace_bytes": (C.c_size_t, [C.POINTER(RouterDesc), C.c_int32]),
+    "fupr_moe_route": (C.c_int32, [C.POINTER(RouterDesc), _M, _V, _V, _V, _V, _V, _V, C.c_size_t, _V]),
+    "fupr_moe_combine": (C.c_int32, [_M, _V, _V, C.c_int32, _M, _M, _V]),
 }
 for _name, (_res, _args) in SIGNATURES.items():
     _fn = getattr(_lib, _name)
@@ -464,6 +499,183 @@ def fupr_tuning_set(name, value):
     """value: None (back to automatic), or anything str() turns into the switch's text."""
     v = None if value is None else str(value).encode()
     _check(_lib.fupr_tuning_set(name.encode(), v), "fupr_tuning_set")
+
+
+# ---- feed-forward layers ---------------------------------------------------------
+# Matrices are torch CUDA tensors whose last dimension is contiguous (a view of wider rows is one).
+
+_DT_OF = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def _dt_of(t, where):
+    dt = _DT_OF.get(t.dtype)
+    if dt is None or not t.is_cuda:
+        raise FuprError(ERR_DTYPE, where)
+    return dt
+
+
+def matrix(t, where="matrix"):
+    """A 2-D torch CUDA tensor as the C struct.  A single row's stride says nothing to torch: it becomes its width
+    rounded up to the alignment rule."""
+    dt = _dt_of(t, where)
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise FuprError(ERR_SHAPE, where)
+    rows, cols = t.shape
+    stride = t.stride(0) if rows > 1 else min_c_stride(cols, dt)
+    return Matrix.from_buffer_copy(_MATRIX(rows, cols, stride, dt, t.data_ptr()))
+
+
+def _vector(t, dtype, n, where):
+    """The address of a contiguous torch CUDA vector of n elements (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_cuda:
+        raise FuprError(ERR_DTYPE, where)
+    if t.numel() != n or not t.is_contiguous():
+        raise FuprError(ERR_SHAPE, where)
+    return t.data_ptr()
+
+
+def _zeros(nbytes, device):
+    return torch.zeros(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+class Linear:
+    """A fupr_linear and the tensors that it points into: w, w_up N x K, bias, bias_up N floats."""
+
+    def __init__(self, w, bias=None, w_up=None, bias_up=None, act=0):
+        self._keep = (w, w_up, bias, bias_up)
+        self.device = w.device
+        m = matrix(w, "Linear")
+        if w_up is not None:
+            u = matrix(w_up, "Linear")
+            if u.dt != m.dt:
+                raise FuprError(ERR_DTYPE, "Linear")
+            if (u.rows, u.cols, u.stride) != (m.rows, m.cols, m.stride):
+                raise FuprError(ERR_SHAPE, "Linear")
+        self.struct = LinearDesc(m.rows, m.cols, m.dt, int(act), m.stride, m.ptr,
+                                 None if w_up is None else w_up.data_ptr(),
+                                 _vector(bias, torch.float32, m.rows, "Linear"),
+                                 _vector(bias_up, torch.float32, m.rows, "Linear"))
+        self._ref = C.byref(self.struct)
+
+    def workspace_bytes(self, rows):
+        return int(_lib.fupr_linear_workspace_bytes(self._ref, int(rows)))
+
+    def workspace(self, rows):
+        """A workspace for calls of at most that many rows, as they expect it first (None: they need none)."""
+        return _zeros(self.workspace_bytes(rows), self.device)
+
+
+class ExpertLinear:
+    """A fupr_expert_linear and its tensors: w, w_up E x N x K, bias, bias_up E x N, n_len, k_len E int32."""
+
+    def __init__(self, w, bias=None, w_up=None, bias_up=None, act=0, n_len=None, k_len=None):
+        where = "ExpertLinear"
+        self._keep = (w, w_up, bias, bias_up, n_len, k_len)
+        self.device = w.device
+        if w.dim() != 3:
+            raise FuprError(ERR_SHAPE, where)
+        E, n, _ = w.shape
+        m = matrix(w[0], where)
+        if w_up is not None:
+            if w_up.dtype != w.dtype:
+                raise FuprError(ERR_DTYPE, where)
+            if w_up.shape != w.shape or w_up.stride() != w.stride():
+                raise FuprError(ERR_SHAPE, where)
+        one = LinearDesc(n, m.cols, m.dt, int(act), m.stride, m.ptr, None if w_up is None else w_up.data_ptr(),
+                         _vector(bias, torch.float32, E * n, where), _vector(bias_up, torch.float32, E * n, where))
+        self.struct = ExpertLinearDesc(one, E, w.stride(0), _vector(n_len, torch.int32, E, where),
+                                       _vector(k_len, torch.int32, E, where))
+        self._ref = C.byref(self.struct)
+
+    def workspace_bytes(self, rows):
+        return int(_lib.fupr_expert_linear_workspace_bytes(self._ref, int(rows)))
+
+    def workspace(self, rows):
+        return _zeros(self.workspace_bytes(rows), self.device)
+
+
+class RoutePlan:
+    """What fupr_moe_route writes for `tokens` tokens, and its workspace."""
+
+    def __init__(self, router, tokens, device):
+        E, k = router.struct.E, router.struct.top_k
+        self.ids = torch.empty((tokens, k), dtype=torch.int32, device=device)
+        self.weights = torch.empty((tokens, k), dtype=torch.float32, device=device)
+        self.offsets = torch.zeros(E + 1, dtype=torch.int32, device=device)
+        self.src = torch.empty(tokens * k, dtype=torch.int32, device=device)
+        self.pos = torch.empty((tokens, k), dtype=torch.int32, device=device)
+        self.ws = _zeros(router.workspace_bytes(tokens), device)
+        self.tokens = tokens
+
+
+class Router:
+    """A fupr_router and its tensors: keep E uint8, select_bias E floats."""
+
+    def __init__(self, experts, top_k, score=0, renormalise=True, scale=1.0, keep=None, select_bias=None):
+        self._keep = (keep, select_bias)
+        self.struct = RouterDesc(int(experts), int(top_k), int(score), int(renormalise), float(scale),
+                                 _vector(keep, torch.uint8, experts, "Router"),
+                                 _vector(select_bias, torch.float32, experts, "Router"))
+        self._ref = C.byref(self.struct)
+
+    def workspace_bytes(self, tokens):
+        return int(_lib.fupr_moe_route_workspace_bytes(self._ref, int(tokens)))
+
+    def plan(self, tokens, device="cuda:0"):
+        return RoutePlan(self, int(tokens), device)
+
+
+def _ws(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+
+
+def fupr_linear_fused(op, x, y, res=None, workspace=None, stream=None):
+    """op: Linear; x, y, res: matrices; y is written."""
+    where = "fupr_linear_fused"
+    ptr, nbytes = _ws(workspace)
+    st = _lib.fupr_linear_fused(op._ref, C.byref(matrix(x, where)), None if res is None else C.byref(matrix(res, where)),
+                                C.byref(matrix(y, where)), ptr, nbytes,
+                                stream if stream is not None else current_stream())
+    _check(st, where)
+
+
+def fupr_expert_linear_fused(op, x, offsets, src, y, workspace=None, stream=None):
+    """op: ExpertLinear; offsets: E + 1 int32; src: None or one int32 per row of y."""
+    where = "fupr_expert_linear_fused"
+    ptr, nbytes = _ws(workspace)
+    st = _lib.fupr_expert_linear_fused(op._ref, C.byref(matrix(x, where)),
+                                       _vector(offsets, torch.int32, op.struct.E + 1, where),
+                                       _vector(src, torch.int32, y.shape[0], where), C.byref(matrix(y, where)), ptr,
+                                       nbytes, stream if stream is not None else current_stream())
+    _check(st, where)
+
+
+def fupr_moe_route(router, logits, plan, stream=None):
+    """router: Router; logits: T x E; plan: a RoutePlan of T tokens, which is written."""
+    where = "fupr_moe_route"
+    if logits.shape[0] != plan.tokens or plan.ids.shape[1] != router.struct.top_k \
+            or plan.offsets.numel() != router.struct.E + 1:
+        raise FuprError(ERR_SHAPE, where)
+    ptr, nbytes = _ws(plan.ws)
+    st = _lib.fupr_moe_route(router._ref, C.byref(matrix(logits, where)), plan.ids.data_ptr(), plan.weights.data_ptr(),
+                             plan.offsets.data_ptr(), plan.src.data_ptr(), plan.pos.data_ptr(), ptr, nbytes,
+                             stream if stream is not None else current_stream())
+    _check(st, where)
+
+
+def fupr_moe_combine(y, pos, weights, res, out, stream=None):
+    """out[t] = (res[t] +) sum_j weights[t, j] * y[pos[t, j]]; pos, weights: T x top_k."""
+    where = "fupr_moe_combine"
+    if pos.dim() != 2 or weights.shape != pos.shape or pos.shape[0] != out.shape[0]:
+        raise FuprError(ERR_SHAPE, where)
+    n = pos.numel()
+    st = _lib.fupr_moe_combine(C.byref(matrix(y, where)), _vector(pos, torch.int32, n, where),
+                               _vector(weights, torch.float32, n, where), pos.shape[1],
+                               None if res is None else C.byref(matrix(res, where)), C.byref(matrix(out, where)),
+                               stream if stream is not None else current_stream())
+    _check(st, where)
 
 
 # ---- model ----------------------------------------------------------------------

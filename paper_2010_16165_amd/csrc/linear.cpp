@@ -1,0 +1,165 @@
+// Entry points of the linear layers: argument checks on the host, then one launch.
+#include "linear.h"
+
+#include <cstdint>
+
+namespace fupr {
+namespace {
+
+bool known_type(fupr_dtype dt) { return dt == FUPR_F32 || dt == FUPR_BF16 || dt == FUPR_F16; }
+int64_t bytes_of(fupr_dtype dt) { return dt == FUPR_F32 ? 4 : 2; }
+bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+
+// Rows are addressed with 64 bits from their start on and with 32 bits inside; 2^31 bytes of one row and 2^46 of a
+// whole tensor keep every product below far from overflow.
+constexpr int64_t kMostStride = int64_t(1) << 28;
+constexpr int64_t kMostElements = int64_t(1) << 44;
+
+fupr_status check_stride(int64_t stride, int64_t cols, int64_t rows, fupr_dtype dt) {
+  if (stride < cols) return FUPR_ERR_SHAPE;
+  if (stride & (16 / bytes_of(dt) - 1)) return FUPR_ERR_ALIGN;
+  if (stride > kMostStride || (rows > 0 && stride > kMostElements / rows)) return FUPR_ERR_LIMIT;
+  return FUPR_OK;
+}
+
+}  // namespace
+
+fupr_status check_matrix(const fupr_matrix& m) {
+  if (!known_type(m.dt)) return FUPR_ERR_DTYPE;
+  if (m.rows < 0 || m.cols < 1) return FUPR_ERR_SHAPE;
+  if (m.rows > 0 && !m.ptr) return FUPR_ERR_NULL;
+  if (misaligned(m.ptr)) return FUPR_ERR_ALIGN;
+  return check_stride(m.stride, m.cols, m.rows, m.dt);
+}
+
+// Whether the two share an element's byte.  Matrices side by side in the rows of one buffer (one stride, other columns)
+// do not; between different strides only the extents are compared.
+bool matrices_overlap(const fupr_matrix& a, const fupr_matrix& b) {
+  if (a.rows == 0 || b.rows == 0) return false;
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.ptr), pb = reinterpret_cast<uintptr_t>(b.ptr);
+  const uintptr_t sa = (uintptr_t)(a.stride * bytes_of(a.dt)), sb = (uintptr_t)(b.stride * bytes_of(b.dt));
+  const uintptr_t wa = (uintptr_t)(a.cols * bytes_of(a.dt)), wb = (uintptr_t)(b.cols * bytes_of(b.dt));
+  if (pa >= pb + (b.rows - 1) * sb + wb || pb >= pa + (a.rows - 1) * sa + wa) return false;
+  if (sa != sb) return true;
+  const uintptr_t off = pb >= pa ? (pb - pa) % sa : (sa - (pa - pb) % sa) % sa;   // of b's columns in a's rows
+  return off < wa || off + wb > sa;
+}
+
+bool same_matrix(const fupr_matrix& a, const fupr_matrix& b) {
+  return a.ptr == b.ptr && a.stride == b.stride && a.dt == b.dt && a.rows == b.rows && a.cols == b.cols;
+}
+
+namespace {
+
+fupr_status check_layer(const fupr_linear& op, int64_t experts, int64_t expert_stride) {
+  if (!known_type(op.dt)) return FUPR_ERR_DTYPE;
+  if (op.N < 1 || op.K < 1) return FUPR_ERR_SHAPE;
+  if (op.act < FUPR_ACT_NONE || op.act > FUPR_ACT_GELU_TANH || (op.bias_up && !op.w_up)) return FUPR_ERR_ARG;
+  if (!op.w) return FUPR_ERR_NULL;
+  if (misaligned(op.w) || misaligned(op.w_up)) return FUPR_ERR_ALIGN;
+  if ((reinterpret_cast<uintptr_t>(op.bias) | reinterpret_cast<uintptr_t>(op.bias_up)) & 3) return FUPR_ERR_ALIGN;
+  const fupr_status st = check_stride(op.w_stride, op.K, op.N, op.dt);
+  if (st != FUPR_OK) return st;
+  if (experts > 1) {
+    if (expert_stride < 0) return FUPR_ERR_SHAPE;
+    if (expert_stride & (16 / bytes_of(op.dt) - 1)) return FUPR_ERR_ALIGN;
+    if (expert_stride > kMostElements / experts) return FUPR_ERR_LIMIT;
+  }
+  return FUPR_OK;
+}
+
+// Whether y touches the extent from the first to the last weight of all experts.
+bool overlaps_weights(const fupr_matrix& y, const fupr_linear& op, const void* w, int64_t experts, int64_t expert_stride) {
+  if (!w || y.rows == 0) return false;
+  const int64_t n = (experts > 1 ? (experts - 1) * expert_stride : 0) + (op.N - 1) * op.w_stride + op.K;
+  const uintptr_t pw = reinterpret_cast<uintptr_t>(w), py = reinterpret_cast<uintptr_t>(y.ptr);
+  return pw < py + (uintptr_t)(((y.rows - 1) * y.stride + y.cols) * bytes_of(y.dt)) &&
+         py < pw + (uintptr_t)(n * bytes_of(op.dt));
+}
+
+fupr_status run_linear(const fupr_linear& op, int32_t E, int64_t expert_stride, const int32_t* n_len,
+                       const int32_t* k_len, const fupr_matrix& x, const int32_t* offsets, const int32_t* src,
+                       const fupr_matrix* res, const fupr_matrix& y, void* workspace, size_t workspace_bytes,
+                       size_t needed, void* stream) {
+  fupr_status st = check_layer(op, E, expert_stride);
+  if (st != FUPR_OK) return st;
+  if ((st = check_matrix(x)) != FUPR_OK || (st = check_matrix(y)) != FUPR_OK) return st;
+  if (res && (st = check_matrix(*res)) != FUPR_OK) return st;
+  if (x.dt != op.dt || (y.dt != op.dt && y.dt != FUPR_F32) || (res && res->dt != y.dt)) return FUPR_ERR_DTYPE;
+  if (x.cols != op.K || y.cols != op.N || (!src && x.rows != y.rows)) return FUPR_ERR_SHAPE;
+  if (src && x.rows < 1 && y.rows > 0) return FUPR_ERR_SHAPE;
+  if (res && (res->rows != y.rows || res->cols != y.cols)) return FUPR_ERR_SHAPE;
+  if ((reinterpret_cast<uintptr_t>(offsets) | reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(n_len) |
+       reinterpret_cast<uintptr_t>(k_len)) & 3)
+    return FUPR_ERR_ALIGN;
+  if (matrices_overlap(x, y) || overlaps_weights(y, op, op.w, E, expert_stride) ||
+      overlaps_weights(y, op, op.w_up, E, expert_stride) ||
+      (res && matrices_overlap(*res, y) && !same_matrix(*res, y)))
+    return FUPR_ERR_ARG;
+  if (needed > 0 && (!workspace || workspace_bytes < needed || (reinterpret_cast<uintptr_t>(workspace) & 255)))
+    return FUPR_ERR_WORKSPACE;
+  if (y.rows == 0) return FUPR_OK;
+  LinearParams p{};
+  const int64_t es = bytes_of(op.dt), ys = bytes_of(y.dt);
+  p.x = (const char*)x.ptr;
+  p.w = (const char*)op.w;
+  p.w_up = (const char*)op.w_up;
+  p.bias = op.bias;
+  p.bias_up = op.bias_up;
+  p.res = res ? (const char*)res->ptr : nullptr;
+  p.y = (char*)y.ptr;
+  p.x_stride = x.stride * es;
+  p.w_stride = op.w_stride * es;
+  p.w_expert = expert_stride * es;
+  p.res_stride = res ? res->stride * ys : 0;
+  p.y_stride = y.stride * ys;
+  p.offsets = offsets;
+  p.src = src;
+  p.n_len = n_len;
+  p.k_len = k_len;
+  p.M = y.rows;
+  p.N = op.N;
+  p.K = op.K;
+  p.E = E;
+  p.x_rows = x.rows;
+  p.act = op.act;
+  p.y_f32 = y.dt == FUPR_F32;
+  return launch_linear_tile(p, op.dt, stream);
+}
+
+}  // namespace
+}  // namespace fupr
+
+using namespace fupr;
+
+extern "C" {
+
+size_t fupr_linear_workspace_bytes(const fupr_linear* op, int32_t rows) {
+  (void)op;
+  (void)rows;
+  return 0;
+}
+
+fupr_status fupr_linear_fused(const fupr_linear* op, const fupr_matrix* x, const fupr_matrix* res, const fupr_matrix* y,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  if (!op || !x || !y) return FUPR_ERR_NULL;
+  return run_linear(*op, 1, 0, nullptr, nullptr, *x, nullptr, nullptr, res, *y, workspace, workspace_bytes,
+                    fupr_linear_workspace_bytes(op, y->rows), stream);
+}
+
+size_t fupr_expert_linear_workspace_bytes(const fupr_expert_linear* op, int32_t rows) {
+  (void)op;
+  (void)rows;
+  return 0;
+}
+
+fupr_status fupr_expert_linear_fused(const fupr_expert_linear* op, const fupr_matrix* x, const int32_t* offsets,
+                                     const int32_t* src, const fupr_matrix* y, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+  if (!op || !x || !y || !offsets) return FUPR_ERR_NULL;
+  if (op->E < 1) return FUPR_ERR_SHAPE;
+  return run_linear(op->one, op->E, op->w_expert_stride, op->n_len, op->k_len, *x, offsets, src, nullptr, *y, workspace,
+                    workspace_bytes, fupr_expert_linear_workspace_bytes(op, y->rows), stream);
+}
+
+}  // extern "C"

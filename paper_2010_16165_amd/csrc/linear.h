@@ -1,0 +1,38 @@
+// Internal: arguments of the kernels behind fupr_linear_fused and fupr_expert_linear_fused.
+#pragma once
+#include <cstdint>
+
+#include "fupr.h"
+
+namespace fupr {
+
+// One layer, or E of them with rows offsets[e] .. offsets[e + 1] - 1 each.  Strides are in bytes.
+struct LinearParams {
+  const char* x;
+  const char* w;
+  const char* w_up;        // nullptr: not gated
+  const float* bias;       // expert e: + e * N
+  const float* bias_up;
+  const char* res;
+  char* y;
+  int64_t x_stride, w_stride, w_expert, res_stride, y_stride;
+  const int32_t* offsets;  // nullptr: one layer
+  const int32_t* src;      // nullptr: row r reads row r of x
+  const int32_t* n_len;    // nullptr: N
+  const int32_t* k_len;    // nullptr: K
+  int M, N, K, E;          // M: rows of y
+  int x_rows;
+  int act;
+  int y_f32;               // y and res are fp32, whatever the type of x and w
+  int m_tiles, n_tiles;    // of the launch: an upper bound on the row tiles of all experts
+};
+
+// linear_tile.hip: tiles of rows and filters staged through LDS.
+fupr_status launch_linear_tile(LinearParams p, fupr_dtype dt, void* stream);
+
+// linear.cpp: argument checks that the entry points share.
+fupr_status check_matrix(const fupr_matrix& m);
+bool matrices_overlap(const fupr_matrix& a, const fupr_matrix& b);
+bool same_matrix(const fupr_matrix& a, const fupr_matrix& b);
+
+}  // namespace fupr

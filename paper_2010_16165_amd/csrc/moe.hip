@@ -1,0 +1,462 @@
+// The router of a mixture of experts and the weighted sum of its experts' results.
+//
+// Choosing: a group of LPT lanes has one token, each lane V of its logits in registers; top_k times the group takes
+// the largest key among its lanes (ties: lowest expert) and strikes it out.  Keys are the logits themselves where no
+// bias is added - softmax and sigmoid are monotonic, so no rounding of theirs decides - and score + bias in fp64 where
+// one is, because two scores may lie closer than fp32 tells apart.
+//
+// Ordering rows by expert, then token: for 64 tokens and an expert one 64-bit word says which of them chose it (atomic
+// OR in LDS: no order of arrival shows in it), so a slot's place is a count of bits below its own.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "device_utils.h"
+#include "linear.h"
+
+namespace fupr {
+
+fupr_status launch_status(const char* what);
+
+namespace {
+
+constexpr int kMostExperts = 1024, kMostChosen = 16;
+constexpr int kBlockTokens = 256;   // tokens of a workgroup: four groups of 64
+constexpr int kGroups = kBlockTokens / 64;
+
+struct RouteParams {
+  const char* logits;
+  int64_t stride;            // bytes
+  int dt, T, E, k;
+  int sigmoid, renorm;
+  float scale;
+  const uint8_t* keep;
+  const float* bias;
+  int32_t *ids, *offsets, *src, *pos;
+  float* weights;
+  int32_t* counts;           // [workgroups][E]: the workspace
+  int blocks;
+};
+
+__device__ __forceinline__ float logit_at(const RouteParams& p, int64_t token, int e) {
+  const char* row = p.logits + token * p.stride;
+  if (p.dt == FUPR_F32) return reinterpret_cast<const float*>(row)[e];
+  const uint16_t h = reinterpret_cast<const uint16_t*>(row)[e];
+  return p.dt == FUPR_BF16 ? to_float<true>(h) : to_float<false>(h);
+}
+
+// Keys as unsigned numbers in the same order; 0: not to be chosen (-inf), all ones: NaN.
+__device__ __forceinline__ uint64_t key_of(float v) {
+  if (v != v) return ~0ull >> 32;
+  if (v == -__builtin_inff()) return 0;
+  const uint32_t b = __float_as_uint(v + 0.f);   // (-0 and 0 are equal)
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t key_of(double v) {
+  if (v != v) return ~0ull;
+  if (v == -__builtin_inf()) return 0;
+  const uint64_t b = (uint64_t)__double_as_longlong(v + 0.0);
+  return b >> 63 ? ~b : b | 1ull << 63;
+}
+
+template <int LPT>
+__device__ __forceinline__ float group_max(float v) {
+#pragma unroll
+  for (int d = 1; d < LPT; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+template <int LPT, class F>
+__device__ __forceinline__ F group_sum(F v) {
+#pragma unroll
+  for (int d = 1; d < LPT; d *= 2) v += __shfl_xor(v, d);
+  return v;
+}
+
+// The chosen experts of one token by a group of LPT lanes; lane j < k of the group returns the j-th (or -1) and its
+// weight.
+template <int LPT, int V>
+__device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int sub, int& id, float& weight) {
+  float l[V];
+  uint64_t key[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int e = i * LPT + sub;
+    l[i] = e < p.E && !(p.keep && p.keep[e] == 0) ? logit_at(p, token, e) : -__builtin_inff();
+  }
+  // softmax: the largest logit and the sum of exponentials (an expert that does not exist has e^-inf = 0)
+  float most = -__builtin_inff(), sum = 0.f;
+  if (!p.sigmoid) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) most = fmaxf(most, l[i]);
+    most = group_max<LPT>(most);
+    if (most == -__builtin_inff()) most = 0.f;   // no expert at all
+#pragma unroll
+    for (int i = 0; i < V; ++i) sum += expf(l[i] - most);
+    sum = group_sum<LPT>(sum);
+  }
+  if (p.bias) {
+    double wide[V], total = 0.0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      wide[i] = p.sigmoid ? 1.0 / (1.0 + exp(-(double)l[i])) : exp((double)l[i] - (double)most);
+      total += wide[i];
+    }
+    if (!p.sigmoid) total = group_sum<LPT>(total);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int e = i * LPT + sub;
+      const double s = p.sigmoid ? wide[i] : wide[i] / total;
+      key[i] = l[i] == -__builtin_inff() ? 0 : key_of(s + (double)p.bias[min(e, p.E - 1)]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = key_of(l[i]);
+  }
+  id = -1;
+  for (int j = 0; j < p.k; ++j) {
+    uint64_t best = 0;
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (key[i] > best) {   // (ascending experts: the first of equals stays)
+        best = key[i];
+        at = i * LPT + sub;
+      }
+#pragma unroll
+    for (int d = 1; d < LPT; d *= 2) {
+      const uint64_t other = __shfl_xor(best, d);
+      const int there = __shfl_xor(at, d);
+      if (other > best || (other == best && there < at)) {
+        best = other;
+        at = there;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i * LPT + sub == at) key[i] = 0;
+    if (sub == j % LPT && best != 0) id = at;
+  }
+  float score = 0.f;
+  if (id >= 0) {
+    const float v = logit_at(p, token, id);
+    score = p.sigmoid ? 1.f / (1.f + expf(-v)) : expf(v - most) / sum;
+  }
+  const float all = p.renorm ? group_sum<LPT>(score) : 1.f;
+  weight = id >= 0 ? p.scale * (p.renorm ? score / all : score) : 0.f;
+}
+
+// The tokens of one workgroup: ids and weights to memory, and for each 64 of them and each expert who chose it.
+template <int LPT, int V>
+__device__ __forceinline__ void choose_block(const RouteParams& p, int64_t t0, uint64_t* who) {
+  constexpr int kPer = 64 / LPT;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, sub = lane % LPT;
+  for (int i = threadIdx.x; i < kGroups * p.E; i += blockDim.x) who[i] = 0;
+  __syncthreads();
+  for (int at = wave * kPer; at < kBlockTokens; at += waves * kPer) {
+    const int in = at + lane / LPT;
+    const int64_t token = t0 + in;
+    int id;
+    float weight;
+    choose<LPT, V>(p, min(token, (int64_t)p.T - 1), sub, id, weight);
+    if (token < p.T && sub < p.k) {
+      p.ids[token * p.k + sub] = id;
+      p.weights[token * p.k + sub] = weight;
+      if (id >= 0) atomicOr((unsigned long long*)&who[(in >> 6) * p.E + id], 1ull << (in & 63));
+    }
+  }
+  __syncthreads();
+}
+
+// The places of the block's slots.  first: in LDS, the row at which the block's part of each expert begins.
+__device__ __forceinline__ void place_block(const RouteParams& p, int64_t t0, const uint64_t* who, const int* first) {
+  const int tokens = (int)min((int64_t)kBlockTokens, p.T - t0);
+  for (int s = threadIdx.x; s < tokens * p.k; s += blockDim.x) {
+    const int in = s / p.k;
+    const int64_t slot = t0 * p.k + s;
+    const int id = p.ids[slot];
+    int at = -1;
+    if (id >= 0 && id < p.E) {
+      at = first[id];
+      for (int g = 0; g < (in >> 6); ++g) at += __popcll(who[g * p.E + id]);
+      at += __popcll(who[(in >> 6) * p.E + id] & ((1ull << (in & 63)) - 1));
+      p.src[at] = (int)(t0 + in);
+    }
+    p.pos[slot] = at;
+  }
+}
+
+// counts[0 .. E) in LDS -> their exclusive prefix sums in first[0 .. E), the total in first[E].
+__device__ __forceinline__ void prefix_experts(int E, const int* counts, int* first) {
+  if (threadIdx.x < 64) {
+    int before = 0;
+    for (int e0 = 0; e0 < E; e0 += 64) {
+      const int e = e0 + threadIdx.x, own = e < E ? counts[e] : 0;
+      int v = own;
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(v, d);
+        if ((int)threadIdx.x >= d) v += o;
+      }
+      if (e < E) first[e] = before + v - own;
+      before += __shfl(v, 63);
+    }
+    if (threadIdx.x == 0) first[E] = before;
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ int block_count(const uint64_t* who, int E, int e) {
+  int n = 0;
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) n += __popcll(who[g * E + e]);
+  return n;
+}
+
+// ONE: the only workgroup, so the rows are ordered at once.
+template <int LPT, int V, bool ONE>
+__global__ __launch_bounds__(1024) void route_choose_kernel(RouteParams p) {
+  __shared__ uint64_t who[kGroups * kMostExperts];
+  __shared__ int counts[kMostExperts], first[kMostExperts + 1];
+  const int64_t t0 = (int64_t)blockIdx.x * kBlockTokens;
+  choose_block<LPT, V>(p, t0, who);
+  for (int e = threadIdx.x; e < p.E; e += blockDim.x) {
+    const int n = block_count(who, p.E, e);
+    if constexpr (ONE) counts[e] = n;
+    else p.counts[(int64_t)blockIdx.x * p.E + e] = n;
+  }
+  if constexpr (ONE) {
+    __syncthreads();
+    prefix_experts(p.E, counts, first);
+    for (int e = threadIdx.x; e <= p.E; e += blockDim.x) p.offsets[e] = first[e];
+    for (int r = first[p.E] + threadIdx.x; r < p.T * p.k; r += blockDim.x) p.src[r] = -1;
+    place_block(p, 0, who, first);
+  }
+}
+
+// The second launch of many tokens: every workgroup adds up how many rows each expert has before its own.
+__global__ __launch_bounds__(1024) void route_place_kernel(RouteParams p) {
+  __shared__ uint64_t who[kGroups * kMostExperts];
+  __shared__ int all[kMostExperts], mine[kMostExperts], first[kMostExperts + 1];
+  const int64_t t0 = (int64_t)blockIdx.x * kBlockTokens;
+  const int tokens = (int)min((int64_t)kBlockTokens, p.T - t0);
+  for (int i = threadIdx.x; i < kGroups * p.E; i += blockDim.x) who[i] = 0;
+  for (int e = threadIdx.x; e < p.E; e += blockDim.x) all[e] = mine[e] = 0;
+  __syncthreads();
+  // integer sums: the order in which they are added does not show
+  const int parts = max(1, (int)blockDim.x / p.E);
+  for (int i = threadIdx.x; i < parts * p.E; i += blockDim.x) {
+    const int part = i / p.E, e = i - part * p.E;
+    int before = 0, total = 0;
+    for (int b = part; b < p.blocks; b += parts) {
+      const int n = p.counts[(int64_t)b * p.E + e];
+      total += n;
+      if (b < (int)blockIdx.x) before += n;
+    }
+    atomicAdd(&all[e], total);
+    atomicAdd(&mine[e], before);
+  }
+  for (int s = threadIdx.x; s < tokens * p.k; s += blockDim.x) {
+    const int id = p.ids[t0 * p.k + s], in = s / p.k;
+    if (id >= 0 && id < p.E) atomicOr((unsigned long long*)&who[(in >> 6) * p.E + id], 1ull << (in & 63));
+  }
+  __syncthreads();
+  prefix_experts(p.E, all, first);
+  const int total = first[p.E];
+  if (blockIdx.x == 0)
+    for (int e = threadIdx.x; e <= p.E; e += blockDim.x) p.offsets[e] = first[e];
+  __syncthreads();
+  for (int e = threadIdx.x; e < p.E; e += blockDim.x) first[e] += mine[e];
+  __syncthreads();
+  const int64_t end = min((t0 + kBlockTokens) * p.k, (int64_t)p.T * p.k);
+  for (int64_t r = max((int64_t)total, t0 * p.k) + threadIdx.x; r < end; r += blockDim.x) p.src[r] = -1;
+  place_block(p, t0, who, first);
+}
+
+template <int LPT, int V>
+void launch_route_as(const RouteParams& p, hipStream_t st) {
+  const int tokens = std::min(p.T, kBlockTokens);
+  const int waves = std::min(16, (tokens * LPT + 63) / 64);
+  if (p.blocks == 1) {
+    route_choose_kernel<LPT, V, true><<<dim3(1), dim3(waves * 64), 0, st>>>(p);
+  } else {
+    route_choose_kernel<LPT, V, false><<<dim3(p.blocks), dim3(1024), 0, st>>>(p);
+    route_place_kernel<<<dim3(p.blocks), dim3(1024), 0, st>>>(p);
+  }
+}
+
+fupr_status check_router(const fupr_router& r) {
+  if (r.E < 1 || r.top_k < 1 || r.top_k > r.E) return FUPR_ERR_SHAPE;
+  if (r.E > kMostExperts || r.top_k > kMostChosen) return FUPR_ERR_LIMIT;
+  if ((r.score != FUPR_SCORE_SOFTMAX && r.score != FUPR_SCORE_SIGMOID) || (r.renormalise != 0 && r.renormalise != 1))
+    return FUPR_ERR_ARG;
+  if (reinterpret_cast<uintptr_t>(r.select_bias) & 3) return FUPR_ERR_ALIGN;
+  return FUPR_OK;
+}
+
+int route_blocks(int T) { return (int)(((int64_t)T + kBlockTokens - 1) / kBlockTokens); }
+
+// ---- weighted sum -----------------------------------------------------------
+
+struct CombineParams {
+  const char* y;
+  const char* res;
+  char* out;
+  int64_t y_stride, res_stride, out_stride;   // bytes
+  const int32_t* pos;
+  const float* weights;
+  int T, k, N, rows, chunks;   // chunks: 16-byte pieces of a row
+};
+
+// A lane has one 16-byte piece of a row of out; the pieces of the chosen rows are asked for four at a time.
+template <int TY>
+__global__ __launch_bounds__(256) void combine_kernel(CombineParams p) {
+  constexpr int EL = TY == FUPR_F32 ? 4 : 8;
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t t = at / p.chunks;
+  const int c = (int)(at - t * p.chunks);
+  if (t >= p.T) return;
+  const int left = p.N - c * EL;
+  float sum[EL];
+  auto add = [&](const uint4& v, float w) {
+    const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < EL; ++i) {
+      float f;
+      if constexpr (TY == FUPR_F32) f = __uint_as_float(d[i]);
+      else f = to_float<TY == FUPR_BF16>((uint16_t)(d[i / 2] >> (i & 1) * 16));
+      sum[i] += w * f;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < EL; ++i) sum[i] = 0.f;
+  // (whole pieces are read, also of a row that ends inside one: a row's memory extends to its stride)
+  if (p.res) add(*reinterpret_cast<const uint4*>(p.res + t * p.res_stride + c * 16), 1.f);
+  for (int j0 = 0; j0 < p.k; j0 += 4) {
+    uint4 v[4];
+    float w[4];
+    bool takes[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = j0 + j < p.k ? p.pos[t * p.k + j0 + j] : -1;
+      takes[j] = r >= 0 && r < p.rows;
+      w[j] = takes[j] ? p.weights[t * p.k + j0 + j] : 0.f;
+      if (takes[j]) v[j] = *reinterpret_cast<const uint4*>(p.y + r * p.y_stride + c * 16);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (takes[j]) add(v[j], w[j]);
+  }
+  char* out = p.out + t * p.out_stride + c * 16;
+  if constexpr (TY == FUPR_F32) {
+    if (left >= EL) *reinterpret_cast<f32x4*>(out) = f32x4{sum[0], sum[1], sum[2], sum[3]};
+    else
+#pragma unroll
+      for (int i = 0; i < EL; ++i)
+        if (i < left) reinterpret_cast<float*>(out)[i] = sum[i];
+  } else {
+    constexpr bool BF = TY == FUPR_BF16;
+    if (left >= EL)
+      *reinterpret_cast<uint4*>(out) = uint4{pack2<BF>(sum[0], sum[1]), pack2<BF>(sum[2], sum[3]),
+                                             pack2<BF>(sum[4], sum[5]), pack2<BF>(sum[6], sum[7])};
+    else
+#pragma unroll
+      for (int i = 0; i < EL; ++i)
+        if (i < left) reinterpret_cast<uint16_t*>(out)[i] = from_float<BF>(sum[i]);
+  }
+}
+
+}  // namespace
+}  // namespace fupr
+
+using namespace fupr;
+
+extern "C" {
+
+size_t fupr_moe_route_workspace_bytes(const fupr_router* router, int32_t tokens) {
+  if (!router || check_router(*router) != FUPR_OK || tokens <= kBlockTokens) return 0;
+  return (size_t)route_blocks(tokens) * (size_t)router->E * sizeof(int32_t);
+}
+
+fupr_status fupr_moe_route(const fupr_router* router, const fupr_matrix* logits, int32_t* ids, float* weights,
+                           int32_t* offsets, int32_t* src, int32_t* pos, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  if (!router || !logits || !offsets) return FUPR_ERR_NULL;
+  fupr_status st = check_router(*router);
+  if (st != FUPR_OK || (st = check_matrix(*logits)) != FUPR_OK) return st;
+  if (logits->cols != router->E) return FUPR_ERR_SHAPE;
+  if (logits->rows > 0 && (!ids || !weights || !src || !pos)) return FUPR_ERR_NULL;
+  for (const void* v : {(const void*)ids, (const void*)weights, (const void*)offsets, (const void*)src, (const void*)pos})
+    if (reinterpret_cast<uintptr_t>(v) & 3) return FUPR_ERR_ALIGN;
+  if ((int64_t)logits->rows * router->top_k > 0x7fffffff - kBlockTokens * kMostChosen) return FUPR_ERR_LIMIT;
+  const size_t needed = fupr_moe_route_workspace_bytes(router, logits->rows);
+  if (needed > 0 && (!workspace || workspace_bytes < needed || (reinterpret_cast<uintptr_t>(workspace) & 255)))
+    return FUPR_ERR_WORKSPACE;
+  if (logits->rows == 0) return FUPR_OK;
+  RouteParams p{};
+  p.logits = (const char*)logits->ptr;
+  p.stride = logits->stride * (logits->dt == FUPR_F32 ? 4 : 2);
+  p.dt = logits->dt;
+  p.T = logits->rows;
+  p.E = router->E;
+  p.k = router->top_k;
+  p.sigmoid = router->score == FUPR_SCORE_SIGMOID;
+  p.renorm = router->renormalise;
+  p.scale = router->scale;
+  p.keep = router->keep;
+  p.bias = router->select_bias;
+  p.ids = ids;
+  p.weights = weights;
+  p.offsets = offsets;
+  p.src = src;
+  p.pos = pos;
+  p.counts = (int32_t*)workspace;
+  p.blocks = route_blocks(p.T);
+  hipStream_t s = (hipStream_t)stream;
+  // the fewest lanes that hold a token's logits in 16 registers each, and one for every expert chosen
+  if (p.E <= 64 && p.k <= 8) launch_route_as<8, 8>(p, s);
+  else if (p.E <= 128 && p.k <= 8) launch_route_as<8, 16>(p, s);
+  else if (p.E <= 256) launch_route_as<16, 16>(p, s);
+  else if (p.E <= 512) launch_route_as<32, 16>(p, s);
+  else launch_route_as<64, 16>(p, s);
+  return launch_status("route_choose_kernel");
+}
+
+fupr_status fupr_moe_combine(const fupr_matrix* y, const int32_t* pos, const float* weights, int32_t top_k,
+                             const fupr_matrix* res, const fupr_matrix* out, void* stream) {
+  if (!y || !out) return FUPR_ERR_NULL;
+  fupr_status st;
+  if ((st = check_matrix(*y)) != FUPR_OK || (st = check_matrix(*out)) != FUPR_OK) return st;
+  if (res && (st = check_matrix(*res)) != FUPR_OK) return st;
+  if (y->dt != out->dt || (res && res->dt != out->dt)) return FUPR_ERR_DTYPE;
+  if (top_k < 1 || y->cols != out->cols || (res && (res->rows != out->rows || res->cols != out->cols))) return FUPR_ERR_SHAPE;
+  if (out->rows > 0 && (!pos || !weights)) return FUPR_ERR_NULL;
+  if ((reinterpret_cast<uintptr_t>(pos) | reinterpret_cast<uintptr_t>(weights)) & 3) return FUPR_ERR_ALIGN;
+  if (matrices_overlap(*y, *out) || (res && matrices_overlap(*res, *out) && !same_matrix(*res, *out))) return FUPR_ERR_ARG;
+  const int64_t es = y->dt == FUPR_F32 ? 4 : 2;
+  CombineParams p{};
+  p.y = (const char*)y->ptr;
+  p.res = res ? (const char*)res->ptr : nullptr;
+  p.out = (char*)out->ptr;
+  p.y_stride = y->stride * es;
+  p.res_stride = res ? res->stride * es : 0;
+  p.out_stride = out->stride * es;
+  p.pos = pos;
+  p.weights = weights;
+  p.T = out->rows;
+  p.k = top_k;
+  p.N = y->cols;
+  p.rows = y->rows;
+  p.chunks = (int)((p.N * es + 15) / 16);
+  const int64_t blocks = ((int64_t)p.T * p.chunks + 255) / 256;
+  if (blocks > 0x7fffffff) return FUPR_ERR_LIMIT;
+  if (p.T == 0) return FUPR_OK;
+  hipStream_t s = (hipStream_t)stream;
+  const dim3 grid((unsigned)blocks);
+  if (y->dt == FUPR_BF16) combine_kernel<FUPR_BF16><<<grid, dim3(256), 0, s>>>(p);
+  else if (y->dt == FUPR_F16) combine_kernel<FUPR_F16><<<grid, dim3(256), 0, s>>>(p);
+  else combine_kernel<FUPR_F32><<<grid, dim3(256), 0, s>>>(p);
+  return launch_status("combine_kernel");
+}
+
+}  // extern "C"

@@ -1,0 +1,101 @@
+"""A mixture-of-experts feed-forward layer whose experts have been pruned (Alg. 1 applied to their hidden units).
+
+An expert is y = down (a(gate x) * (up x)); its hidden units are the filters of gate and up together, and the input
+channels of down.  prune_experts takes the units of lowest norm with the library's own passes, each expert at its own
+rate; ExpertLayer runs the layer on the device:
+
+    logits = router x                  fupr_linear_fused
+    who goes where                     fupr_moe_route
+    h = a(gate x) * (up x)             fupr_expert_linear_fused, on the rows each expert was given
+    y = down h                         fupr_expert_linear_fused, over the units each expert has left
+    out = res + weighted sum of y      fupr_moe_combine
+"""
+from __future__ import annotations
+
+import numpy as np
+import torch
+
+from . import binding as B
+
+
+def prune_experts(gate, up, down, permille, norm=2):
+    """gate, up: E x F x D, down: E x D x F float32; permille: one rate, or one per expert.
+
+    Returns (gate, up, down, widths): each expert's kept units moved to the front, in their order, zeros behind
+    them; the arrays are as wide as the widest expert.  A unit's norm is taken over its gate and up weights."""
+    gate, up, down = (np.asarray(a, dtype=np.float32) for a in (gate, up, down))
+    E, F, D = gate.shape
+    rates = [int(permille)] * E if np.isscalar(permille) else [int(p) for p in permille]
+    if up.shape != (E, F, D) or down.shape != (E, D, F) or len(rates) != E:
+        raise B.FuprError(B.ERR_SHAPE, "prune_experts")
+    kept = []
+    for e in range(E):
+        units = np.concatenate([gate[e], up[e]], axis=1)[:, :, None, None]
+        shape = B.shape_of(units, 1, 0)
+        mask = B.fupr_select_filters(shape, units, norm, B.fupr_prune_count(F, rates[e]))
+        cons = B.conv_shape(D, F, 1, 1, 1, 0)
+        _, thin, _, (back,) = B.fupr_prune(shape, units, None, mask, [cons], [down[e][:, :, None, None]])
+        kept.append((thin[:, :D, 0, 0], thin[:, D:, 0, 0], back[:, :, 0, 0]))
+    widths = np.array([k[0].shape[0] for k in kept], dtype=np.int32)
+    most = int(widths.max())
+    out = [np.zeros((E, most, D), np.float32), np.zeros((E, most, D), np.float32), np.zeros((E, D, most), np.float32)]
+    for e, (g, u, d) in enumerate(kept):
+        out[0][e, :widths[e]], out[1][e, :widths[e]], out[2][e, :, :widths[e]] = g, u, d
+    return (*out, widths)
+
+
+def _rows(a, dtype, device):
+    """An array on the device in rows that start at multiples of 16 bytes."""
+    t = torch.as_tensor(a)
+    unit = 16 // dtype.itemsize
+    out = torch.zeros((*t.shape[:-1], -(-t.shape[-1] // unit) * unit), dtype=dtype, device=device)
+    out[..., :t.shape[-1]] = t.to(device)
+    return out[..., :t.shape[-1]]
+
+
+class ExpertLayer:
+    """router: E x D; gate, up: E x F x D; down: E x D x F; widths: hidden units of each expert (None: F)."""
+
+    def __init__(self, router, gate, up, down, top_k, widths=None, act="silu", score="softmax", renormalise=True,
+                 scale=1.0, keep=None, select_bias=None, dtype=torch.bfloat16, device="cuda:0"):
+        self.dtype, self.device = dtype, device
+        self.E, self.F, self.D = gate.shape
+        if widths is not None:
+            widths = torch.as_tensor(widths).to(device=device, dtype=torch.int32)
+        router, gate, up, down = (_rows(a, dtype, device) for a in (router, gate, up, down))
+        self.logits_op = B.Linear(router)
+        self.router = B.Router(self.E, top_k, B.SCORES[score], renormalise, scale, keep, select_bias)
+        self.up_op = B.ExpertLinear(gate, w_up=up, act=B.ACTIVATIONS[act], n_len=widths)
+        self.down_op = B.ExpertLinear(down, k_len=widths)
+        self.top_k = top_k
+
+    def alloc(self, tokens):
+        """What a pass over that many tokens works in; one per stream that runs the layer."""
+        return LayerBuffers(self, tokens)
+
+    def forward(self, x, out, buf, res=None, stream=None):
+        """out = (res +) the layer's result for the rows of x; out may be res itself.  Enqueued on the stream."""
+        plan = buf.plan
+        B.fupr_linear_fused(self.logits_op, x, buf.logits, None, buf.ws_logits, stream)
+        B.fupr_moe_route(self.router, buf.logits, plan, stream)
+        B.fupr_expert_linear_fused(self.up_op, x, plan.offsets, plan.src, buf.hidden, buf.ws_up, stream)
+        B.fupr_expert_linear_fused(self.down_op, buf.hidden, plan.offsets, None, buf.rows, buf.ws_down, stream)
+        B.fupr_moe_combine(buf.rows, plan.pos, plan.weights, res, out, stream)
+
+
+class LayerBuffers:
+    def __init__(self, layer, tokens):
+        slots, dev = tokens * layer.top_k, layer.device
+
+        def empty(rows, cols, dt):
+            unit = 16 // dt.itemsize
+            return torch.empty((rows, -(-cols // unit) * unit), dtype=dt, device=dev)[:, :cols]
+
+        # logits in fp32: a rounding of theirs would decide between experts
+        self.logits = empty(tokens, layer.E, torch.float32)
+        self.plan = layer.router.plan(tokens, dev)
+        self.hidden = empty(slots, layer.F, layer.dtype)
+        self.rows = empty(slots, layer.D, layer.dtype)
+        self.ws_logits = layer.logits_op.workspace(tokens)
+        self.ws_up = layer.up_op.workspace(slots)
+        self.ws_down = layer.down_op.workspace(slots)
