@@ -762,6 +762,8 @@ void fupr_graph_destroy(fupr_graph* g);
  *   resident_rows = 0                             models made meanwhile: the one-kernel schedule without its
  *                                                 kernel for networks of 3 x 3 convolutions
  *   res_item = "M/FT/nsteps:MTxNT,..."            work-item shapes of the one-kernel schedule
+ *   linear_rows = <rows>                          most rows of a linear layer (of the average expert) for the kernel
+ *                                                 of few rows
  *   debug = 1                                     planner decisions and HIP error text on stderr
  * Errors: NULL, ARG (unknown name, value of 128 characters or more).
  */

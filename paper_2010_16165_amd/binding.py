@@ -123,7 +123,7 @@ _U8 = C.POINTER(C.c_uint8)
 _I32 = C.POINTER(C.c_int32)
 _SH = C.POINTER(ConvShape)
 _T = C.POINTER(Tensor)
-_M = C.POINTER(Matrix)
+_M = C.c_void_p   # the bytes of a Matrix (or its address)
 _V = C.c_void_p
 
 # Every symbol include/fupr.h declares, with its C signature.
@@ -505,31 +505,31 @@ def fupr_tuning_set(name, value):
 # Matrices are torch CUDA tensors whose last dimension is contiguous (a view of wider rows is one).
 
 _DT_OF = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+# what a row's start is aligned to, in elements
+_UNIT_OF = {F32: 4, BF16: 8, F16: 8}
 
 
-def _dt_of(t, where):
+def _matrix(t, where):
+    """A 2-D torch CUDA tensor as the bytes of a fupr_matrix.  A single row's stride says nothing to torch: it becomes
+    its width rounded up to the alignment rule."""
     dt = _DT_OF.get(t.dtype)
     if dt is None or not t.is_cuda:
         raise FuprError(ERR_DTYPE, where)
-    return dt
-
-
-def matrix(t, where="matrix"):
-    """A 2-D torch CUDA tensor as the C struct.  A single row's stride says nothing to torch: it becomes its width
-    rounded up to the alignment rule."""
-    dt = _dt_of(t, where)
-    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or (strides[1] != 1 and shape[1] > 1):
         raise FuprError(ERR_SHAPE, where)
-    rows, cols = t.shape
-    stride = t.stride(0) if rows > 1 else min_c_stride(cols, dt)
-    return Matrix.from_buffer_copy(_MATRIX(rows, cols, stride, dt, t.data_ptr()))
+    rows, cols = shape
+    if rows > 1:
+        return _MATRIX(rows, cols, strides[0], dt, t.data_ptr())
+    unit = _UNIT_OF[dt]
+    return _MATRIX(rows, cols, (cols + unit - 1) // unit * unit, dt, t.data_ptr())
 
 
 def _vector(t, dtype, n, where):
     """The address of a contiguous torch CUDA vector of n elements (None: NULL)."""
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_cuda:
+    if t.dtype is not dtype or not t.is_cuda:
         raise FuprError(ERR_DTYPE, where)
     if t.numel() != n or not t.is_contiguous():
         raise FuprError(ERR_SHAPE, where)
@@ -546,9 +546,9 @@ class Linear:
     def __init__(self, w, bias=None, w_up=None, bias_up=None, act=0):
         self._keep = (w, w_up, bias, bias_up)
         self.device = w.device
-        m = matrix(w, "Linear")
+        m = Matrix.from_buffer_copy(_matrix(w, "Linear"))
         if w_up is not None:
-            u = matrix(w_up, "Linear")
+            u = Matrix.from_buffer_copy(_matrix(w_up, "Linear"))
             if u.dt != m.dt:
                 raise FuprError(ERR_DTYPE, "Linear")
             if (u.rows, u.cols, u.stride) != (m.rows, m.cols, m.stride):
@@ -577,7 +577,7 @@ class ExpertLinear:
         if w.dim() != 3:
             raise FuprError(ERR_SHAPE, where)
         E, n, _ = w.shape
-        m = matrix(w[0], where)
+        m = Matrix.from_buffer_copy(_matrix(w[0], where))
         if w_up is not None:
             if w_up.dtype != w.dtype:
                 raise FuprError(ERR_DTYPE, where)
@@ -627,6 +627,15 @@ class Router:
         return RoutePlan(self, int(tokens), device)
 
 
+def _stream(stream):
+    """The address of a stream handle; None: torch's current stream."""
+    if stream is not None:
+        return stream
+    if torch.cuda.is_initialized():
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return torch.cuda.current_stream().cuda_stream
+
+
 def _ws(workspace):
     return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
 
@@ -635,9 +644,9 @@ def fupr_linear_fused(op, x, y, res=None, workspace=None, stream=None):
     """op: Linear; x, y, res: matrices; y is written."""
     where = "fupr_linear_fused"
     ptr, nbytes = _ws(workspace)
-    st = _lib.fupr_linear_fused(op._ref, C.byref(matrix(x, where)), None if res is None else C.byref(matrix(res, where)),
-                                C.byref(matrix(y, where)), ptr, nbytes,
-                                stream if stream is not None else current_stream())
+    st = _lib.fupr_linear_fused(op._ref, _matrix(x, where), None if res is None else _matrix(res, where),
+                                _matrix(y, where), ptr, nbytes,
+                                _stream(stream))
     _check(st, where)
 
 
@@ -645,10 +654,10 @@ def fupr_expert_linear_fused(op, x, offsets, src, y, workspace=None, stream=None
     """op: ExpertLinear; offsets: E + 1 int32; src: None or one int32 per row of y."""
     where = "fupr_expert_linear_fused"
     ptr, nbytes = _ws(workspace)
-    st = _lib.fupr_expert_linear_fused(op._ref, C.byref(matrix(x, where)),
+    st = _lib.fupr_expert_linear_fused(op._ref, _matrix(x, where),
                                        _vector(offsets, torch.int32, op.struct.E + 1, where),
-                                       _vector(src, torch.int32, y.shape[0], where), C.byref(matrix(y, where)), ptr,
-                                       nbytes, stream if stream is not None else current_stream())
+                                       _vector(src, torch.int32, y.shape[0], where), _matrix(y, where), ptr,
+                                       nbytes, _stream(stream))
     _check(st, where)
 
 
@@ -659,9 +668,9 @@ def fupr_moe_route(router, logits, plan, stream=None):
             or plan.offsets.numel() != router.struct.E + 1:
         raise FuprError(ERR_SHAPE, where)
     ptr, nbytes = _ws(plan.ws)
-    st = _lib.fupr_moe_route(router._ref, C.byref(matrix(logits, where)), plan.ids.data_ptr(), plan.weights.data_ptr(),
+    st = _lib.fupr_moe_route(router._ref, _matrix(logits, where), plan.ids.data_ptr(), plan.weights.data_ptr(),
                              plan.offsets.data_ptr(), plan.src.data_ptr(), plan.pos.data_ptr(), ptr, nbytes,
-                             stream if stream is not None else current_stream())
+                             _stream(stream))
     _check(st, where)
 
 
@@ -671,10 +680,10 @@ def fupr_moe_combine(y, pos, weights, res, out, stream=None):
     if pos.dim() != 2 or weights.shape != pos.shape or pos.shape[0] != out.shape[0]:
         raise FuprError(ERR_SHAPE, where)
     n = pos.numel()
-    st = _lib.fupr_moe_combine(C.byref(matrix(y, where)), _vector(pos, torch.int32, n, where),
+    st = _lib.fupr_moe_combine(_matrix(y, where), _vector(pos, torch.int32, n, where),
                                _vector(weights, torch.float32, n, where), pos.shape[1],
-                               None if res is None else C.byref(matrix(res, where)), C.byref(matrix(out, where)),
-                               stream if stream is not None else current_stream())
+                               None if res is None else _matrix(res, where), _matrix(out, where),
+                               _stream(stream))
     _check(st, where)
 
 

@@ -124,7 +124,7 @@ fupr_status run_linear(const fupr_linear& op, int32_t E, int64_t expert_stride, 
   p.x_rows = x.rows;
   p.act = op.act;
   p.y_f32 = y.dt == FUPR_F32;
-  return launch_linear_tile(p, op.dt, stream);
+  return linear_rows_applies(p, op.dt) ? launch_linear_rows(p, op.dt, stream) : launch_linear_tile(p, op.dt, stream);
 }
 
 }  // namespace

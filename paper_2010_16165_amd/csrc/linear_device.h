@@ -116,6 +116,7 @@ __device__ __forceinline__ void with_activation(int act, F f) {
 // A wave counts 64 experts at a time; an expert's rows are what its two offsets, clamped into 0 .. M, span.
 struct ExpertRows {
   int e, lo, hi, tile;   // tile: of the expert's own
+  int n_len, k_len;
 };
 template <int BM>
 __device__ __forceinline__ int expert_tiles(const LinearParams& p, int e, int& lo, int& hi) {
@@ -149,6 +150,9 @@ __device__ __forceinline__ bool find_expert(const LinearParams& p, int at, int l
   for (int e0 = 0; e0 < p.E; e0 += 64) {
     int lo, hi;
     const int n = expert_tiles<BM>(p, e0 + lane, lo, hi);
+    // (asked for together with the offsets: one latency, not two)
+    const int mine_n = p.n_len && e0 + lane < p.E ? p.n_len[e0 + lane] : p.N;
+    const int mine_k = p.k_len && e0 + lane < p.E ? p.k_len[e0 + lane] : p.K;
     const int upto = before + wave_prefix(n, lane);
     const uint64_t mine = __ballot(at >= upto - n && at < upto);
     if (mine) {
@@ -157,6 +161,8 @@ __device__ __forceinline__ bool find_expert(const LinearParams& p, int at, int l
       out.lo = __builtin_amdgcn_readfirstlane(__shfl(lo, who));
       out.hi = __builtin_amdgcn_readfirstlane(__shfl(hi, who));
       out.tile = __builtin_amdgcn_readfirstlane(at - __shfl(upto - n, who));
+      out.n_len = __builtin_amdgcn_readfirstlane(min(max(__shfl(mine_n, who), 0), p.N));
+      out.k_len = __builtin_amdgcn_readfirstlane(min(max(__shfl(mine_k, who), 0), p.K));
       return true;
     }
     before = __shfl(upto, 63);

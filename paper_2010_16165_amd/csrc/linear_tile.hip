@@ -112,7 +112,7 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
   const bool gated = p.w_up != nullptr;
   const int cols = gated ? BN / 2 : BN;   // of y, in a tile
 
-  int e = 0, lo = 0, hi = p.M, m0, nt;
+  int e = 0, hi = p.M, m0, nt, n_len = p.N, k_len = p.K;
   if (p.offsets) {
     const int at = tile_of_workgroup(blockIdx.x, count_expert_tiles<BM>(p, lane) * p.n_tiles);
     if (at < 0) return;
@@ -121,9 +121,10 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
     nt = at - mt * p.n_tiles;
     if (!find_expert<BM>(p, mt, lane, r)) return;
     e = r.e;
-    lo = r.lo;
     hi = r.hi;
-    m0 = lo + r.tile * BM;
+    m0 = r.lo + r.tile * BM;
+    n_len = r.n_len;
+    k_len = r.k_len;
   } else {
     // strips of eight row tiles: what an XCD holds at one time is about as tall as it is wide
     const int at = tile_of_workgroup(blockIdx.x, p.m_tiles * p.n_tiles);
@@ -134,8 +135,6 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
     m0 = (strip * 8 + in - nt * tall) * BM;
   }
   const int n0 = nt * cols;
-  const int n_len = p.n_len ? min(max(p.n_len[e], 0), p.N) : p.N;
-  const int k_len = p.k_len ? min(max(p.k_len[e], 0), p.K) : p.K;
   const int steps = n0 < n_len ? (k_len + G::per_step - 1) / G::per_step : 0;
 
   // the lane's place in every load: row lane / 8 of eight, chunk (lane & 7) ^ row

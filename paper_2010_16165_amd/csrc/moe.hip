@@ -11,6 +11,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "device_utils.h"
 #include "linear.h"
@@ -22,8 +23,9 @@ fupr_status launch_status(const char* what);
 namespace {
 
 constexpr int kMostExperts = 1024, kMostChosen = 16;
-constexpr int kBlockTokens = 256;   // tokens of a workgroup: four groups of 64
-constexpr int kGroups = kBlockTokens / 64;
+constexpr int kOneTokens = 256;     // up to here one workgroup chooses and orders, in one launch
+constexpr int kManyBlocks = 256;    // from here on workgroups take more than 64 tokens each
+constexpr int kWhoBytes = 48 << 10; // of LDS, for the words that say who chose an expert
 
 struct RouteParams {
   const char* logits;
@@ -36,7 +38,7 @@ struct RouteParams {
   int32_t *ids, *offsets, *src, *pos;
   float* weights;
   int32_t* counts;           // [workgroups][E]: the workspace
-  int blocks;
+  int blocks, groups;        // a workgroup has `groups` times 64 tokens
 };
 
 __device__ __forceinline__ float logit_at(const RouteParams& p, int64_t token, int e) {
@@ -47,8 +49,8 @@ __device__ __forceinline__ float logit_at(const RouteParams& p, int64_t token, i
 }
 
 // Keys as unsigned numbers in the same order; 0: not to be chosen (-inf), all ones: NaN.
-__device__ __forceinline__ uint64_t key_of(float v) {
-  if (v != v) return ~0ull >> 32;
+__device__ __forceinline__ uint32_t key_of(float v) {
+  if (v != v) return ~0u;
   if (v == -__builtin_inff()) return 0;
   const uint32_t b = __float_as_uint(v + 0.f);   // (-0 and 0 are equal)
   return b & 0x80000000u ? ~b : b | 0x80000000u;
@@ -75,10 +77,11 @@ __device__ __forceinline__ F group_sum(F v) {
 
 // The chosen experts of one token by a group of LPT lanes; lane j < k of the group returns the j-th (or -1) and its
 // weight.
-template <int LPT, int V>
+template <int LPT, int V, bool BIASED>
 __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int sub, int& id, float& weight) {
+  typedef typename std::conditional<BIASED, unsigned long long, uint32_t>::type Key;
   float l[V];
-  uint64_t key[V];
+  Key key[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     const int e = i * LPT + sub;
@@ -95,27 +98,25 @@ __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int 
     for (int i = 0; i < V; ++i) sum += expf(l[i] - most);
     sum = group_sum<LPT>(sum);
   }
-  if (p.bias) {
+  if constexpr (BIASED) {
     double wide[V], total = 0.0;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       wide[i] = p.sigmoid ? 1.0 / (1.0 + exp(-(double)l[i])) : exp((double)l[i] - (double)most);
       total += wide[i];
     }
-    if (!p.sigmoid) total = group_sum<LPT>(total);
+    if (p.sigmoid) total = 1.0;
+    else total = group_sum<LPT>(total);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int e = i * LPT + sub;
-      const double s = p.sigmoid ? wide[i] : wide[i] / total;
-      key[i] = l[i] == -__builtin_inff() ? 0 : key_of(s + (double)p.bias[min(e, p.E - 1)]);
-    }
+    for (int i = 0; i < V; ++i)
+      key[i] = l[i] == -__builtin_inff() ? 0 : key_of(wide[i] / total + (double)p.bias[min(i * LPT + sub, p.E - 1)]);
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = key_of(l[i]);
   }
   id = -1;
   for (int j = 0; j < p.k; ++j) {
-    uint64_t best = 0;
+    Key best = 0;
     int at = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -125,7 +126,7 @@ __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int 
       }
 #pragma unroll
     for (int d = 1; d < LPT; d *= 2) {
-      const uint64_t other = __shfl_xor(best, d);
+      const Key other = __shfl_xor(best, d);
       const int there = __shfl_xor(at, d);
       if (other > best || (other == best && there < at)) {
         best = other;
@@ -146,47 +147,42 @@ __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int 
   weight = id >= 0 ? p.scale * (p.renorm ? score / all : score) : 0.f;
 }
 
-// The tokens of one workgroup: ids and weights to memory, and for each 64 of them and each expert who chose it.
-template <int LPT, int V>
-__device__ __forceinline__ void choose_block(const RouteParams& p, int64_t t0, uint64_t* who) {
-  constexpr int kPer = 64 / LPT;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, sub = lane % LPT;
-  for (int i = threadIdx.x; i < kGroups * p.E; i += blockDim.x) who[i] = 0;
-  __syncthreads();
-  for (int at = wave * kPer; at < kBlockTokens; at += waves * kPer) {
-    const int in = at + lane / LPT;
-    const int64_t token = t0 + in;
-    int id;
-    float weight;
-    choose<LPT, V>(p, min(token, (int64_t)p.T - 1), sub, id, weight);
-    if (token < p.T && sub < p.k) {
-      p.ids[token * p.k + sub] = id;
-      p.weights[token * p.k + sub] = weight;
-      if (id >= 0) atomicOr((unsigned long long*)&who[(in >> 6) * p.E + id], 1ull << (in & 63));
-    }
-  }
-  __syncthreads();
+// A workgroup's LDS: who[groups][E], counts[E], first[E + 1] and, where it orders its own tokens, ids[tokens][k].
+struct RouteLds {
+  unsigned long long* who;
+  int *counts, *first, *ids;
+};
+__device__ __forceinline__ RouteLds route_lds(const RouteParams& p) {
+  extern __shared__ unsigned long long route_memory[];
+  RouteLds l;
+  l.who = route_memory;
+  l.counts = reinterpret_cast<int*>(l.who + p.groups * p.E);
+  l.first = l.counts + p.E;
+  l.ids = l.first + p.E + 1;
+  return l;
+}
+size_t route_lds_bytes(const RouteParams& p, bool one) {
+  return (size_t)p.groups * p.E * 8 + (2 * p.E + 1) * 4 + (one ? (size_t)p.T * p.k * 4 : 0);
 }
 
-// The places of the block's slots.  first: in LDS, the row at which the block's part of each expert begins.
-__device__ __forceinline__ void place_block(const RouteParams& p, int64_t t0, const uint64_t* who, const int* first) {
-  const int tokens = (int)min((int64_t)kBlockTokens, p.T - t0);
+// The places of the workgroup's slots, whose experts are ids[0 .. tokens * k).  first: the row at which the workgroup's
+// part of each expert begins.
+__device__ __forceinline__ void place_tokens(const RouteParams& p, int64_t t0, int tokens, const RouteLds& l,
+                                             const int* ids) {
   for (int s = threadIdx.x; s < tokens * p.k; s += blockDim.x) {
-    const int in = s / p.k;
-    const int64_t slot = t0 * p.k + s;
-    const int id = p.ids[slot];
+    const int in = s / p.k, id = ids[s];
     int at = -1;
     if (id >= 0 && id < p.E) {
-      at = first[id];
-      for (int g = 0; g < (in >> 6); ++g) at += __popcll(who[g * p.E + id]);
-      at += __popcll(who[(in >> 6) * p.E + id] & ((1ull << (in & 63)) - 1));
+      at = l.first[id];
+      for (int g = 0; g < (in >> 6); ++g) at += __popcll(l.who[g * p.E + id]);
+      at += __popcll(l.who[(in >> 6) * p.E + id] & ((1ull << (in & 63)) - 1));
       p.src[at] = (int)(t0 + in);
     }
-    p.pos[slot] = at;
+    p.pos[t0 * p.k + s] = at;
   }
 }
 
-// counts[0 .. E) in LDS -> their exclusive prefix sums in first[0 .. E), the total in first[E].
+// counts[0 .. E) -> their exclusive prefix sums in first[0 .. E), the total in first[E].
 __device__ __forceinline__ void prefix_experts(int E, const int* counts, int* first) {
   if (threadIdx.x < 64) {
     int before = 0;
@@ -206,83 +202,100 @@ __device__ __forceinline__ void prefix_experts(int E, const int* counts, int* fi
   __syncthreads();
 }
 
-__device__ __forceinline__ int block_count(const uint64_t* who, int E, int e) {
-  int n = 0;
-#pragma unroll
-  for (int g = 0; g < kGroups; ++g) n += __popcll(who[g * E + e]);
-  return n;
-}
-
 // ONE: the only workgroup, so the rows are ordered at once.
-template <int LPT, int V, bool ONE>
-__global__ __launch_bounds__(1024) void route_choose_kernel(RouteParams p) {
-  __shared__ uint64_t who[kGroups * kMostExperts];
-  __shared__ int counts[kMostExperts], first[kMostExperts + 1];
-  const int64_t t0 = (int64_t)blockIdx.x * kBlockTokens;
-  choose_block<LPT, V>(p, t0, who);
+template <int LPT, int V, bool BIASED, bool ONE>
+__global__ __launch_bounds__(512) void route_choose_kernel(RouteParams p) {
+  constexpr int kPer = 64 / LPT;
+  const RouteLds l = route_lds(p);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, sub = lane % LPT;
+  const int64_t t0 = (int64_t)blockIdx.x * p.groups * 64;
+  const int tokens = (int)min((int64_t)p.groups * 64, p.T - t0);
+  for (int i = threadIdx.x; i < p.groups * p.E; i += blockDim.x) l.who[i] = 0;
+  __syncthreads();
+  for (int at = wave * kPer; at < tokens; at += waves * kPer) {
+    const int in = at + lane / LPT;
+    int id;
+    float weight;
+    choose<LPT, V, BIASED>(p, t0 + min(in, tokens - 1), sub, id, weight);
+    if (in < tokens && sub < p.k) {
+      const int64_t slot = (t0 + in) * p.k + sub;
+      p.ids[slot] = id;
+      p.weights[slot] = weight;
+      if constexpr (ONE) l.ids[in * p.k + sub] = id;
+      if (id >= 0) atomicOr(&l.who[(in >> 6) * p.E + id], 1ull << (in & 63));
+    }
+  }
+  __syncthreads();
   for (int e = threadIdx.x; e < p.E; e += blockDim.x) {
-    const int n = block_count(who, p.E, e);
-    if constexpr (ONE) counts[e] = n;
+    int n = 0;
+    for (int g = 0; g < p.groups; ++g) n += __popcll(l.who[g * p.E + e]);
+    if constexpr (ONE) l.counts[e] = n;
     else p.counts[(int64_t)blockIdx.x * p.E + e] = n;
   }
   if constexpr (ONE) {
     __syncthreads();
-    prefix_experts(p.E, counts, first);
-    for (int e = threadIdx.x; e <= p.E; e += blockDim.x) p.offsets[e] = first[e];
-    for (int r = first[p.E] + threadIdx.x; r < p.T * p.k; r += blockDim.x) p.src[r] = -1;
-    place_block(p, 0, who, first);
+    prefix_experts(p.E, l.counts, l.first);
+    for (int e = threadIdx.x; e <= p.E; e += blockDim.x) p.offsets[e] = l.first[e];
+    for (int r = l.first[p.E] + threadIdx.x; r < p.T * p.k; r += blockDim.x) p.src[r] = -1;
+    place_tokens(p, 0, tokens, l, l.ids);
   }
 }
 
 // The second launch of many tokens: every workgroup adds up how many rows each expert has before its own.
 __global__ __launch_bounds__(1024) void route_place_kernel(RouteParams p) {
-  __shared__ uint64_t who[kGroups * kMostExperts];
-  __shared__ int all[kMostExperts], mine[kMostExperts], first[kMostExperts + 1];
-  const int64_t t0 = (int64_t)blockIdx.x * kBlockTokens;
-  const int tokens = (int)min((int64_t)kBlockTokens, p.T - t0);
-  for (int i = threadIdx.x; i < kGroups * p.E; i += blockDim.x) who[i] = 0;
-  for (int e = threadIdx.x; e < p.E; e += blockDim.x) all[e] = mine[e] = 0;
+  __shared__ int mine[kMostExperts];
+  const RouteLds l = route_lds(p);
+  const int64_t t0 = (int64_t)blockIdx.x * p.groups * 64;
+  const int tokens = (int)min((int64_t)p.groups * 64, p.T - t0);
+  for (int i = threadIdx.x; i < p.groups * p.E; i += blockDim.x) l.who[i] = 0;
+  for (int e = threadIdx.x; e < p.E; e += blockDim.x) l.counts[e] = mine[e] = 0;
   __syncthreads();
   // integer sums: the order in which they are added does not show
   const int parts = max(1, (int)blockDim.x / p.E);
   for (int i = threadIdx.x; i < parts * p.E; i += blockDim.x) {
     const int part = i / p.E, e = i - part * p.E;
     int before = 0, total = 0;
+#pragma unroll 8
     for (int b = part; b < p.blocks; b += parts) {
       const int n = p.counts[(int64_t)b * p.E + e];
       total += n;
-      if (b < (int)blockIdx.x) before += n;
+      before += b < (int)blockIdx.x ? n : 0;
     }
-    atomicAdd(&all[e], total);
+    atomicAdd(&l.counts[e], total);
     atomicAdd(&mine[e], before);
   }
   for (int s = threadIdx.x; s < tokens * p.k; s += blockDim.x) {
     const int id = p.ids[t0 * p.k + s], in = s / p.k;
-    if (id >= 0 && id < p.E) atomicOr((unsigned long long*)&who[(in >> 6) * p.E + id], 1ull << (in & 63));
+    if (id >= 0 && id < p.E) atomicOr(&l.who[(in >> 6) * p.E + id], 1ull << (in & 63));
   }
   __syncthreads();
-  prefix_experts(p.E, all, first);
-  const int total = first[p.E];
+  prefix_experts(p.E, l.counts, l.first);
+  const int total = l.first[p.E];
   if (blockIdx.x == 0)
-    for (int e = threadIdx.x; e <= p.E; e += blockDim.x) p.offsets[e] = first[e];
+    for (int e = threadIdx.x; e <= p.E; e += blockDim.x) p.offsets[e] = l.first[e];
   __syncthreads();
-  for (int e = threadIdx.x; e < p.E; e += blockDim.x) first[e] += mine[e];
+  for (int e = threadIdx.x; e < p.E; e += blockDim.x) l.first[e] += mine[e];
   __syncthreads();
-  const int64_t end = min((t0 + kBlockTokens) * p.k, (int64_t)p.T * p.k);
+  const int64_t end = (t0 + tokens) * p.k;
   for (int64_t r = max((int64_t)total, t0 * p.k) + threadIdx.x; r < end; r += blockDim.x) p.src[r] = -1;
-  place_block(p, t0, who, first);
+  place_tokens(p, t0, tokens, l, p.ids + t0 * p.k);
 }
 
-template <int LPT, int V>
+template <int LPT, int V, bool BIASED>
 void launch_route_as(const RouteParams& p, hipStream_t st) {
-  const int tokens = std::min(p.T, kBlockTokens);
-  const int waves = std::min(16, (tokens * LPT + 63) / 64);
+  const int tokens = std::min(p.T, p.groups * 64);
+  const int waves = std::min(8, (tokens * LPT + 63) / 64);
   if (p.blocks == 1) {
-    route_choose_kernel<LPT, V, true><<<dim3(1), dim3(waves * 64), 0, st>>>(p);
+    route_choose_kernel<LPT, V, BIASED, true><<<dim3(1), dim3(waves * 64), route_lds_bytes(p, true), st>>>(p);
   } else {
-    route_choose_kernel<LPT, V, false><<<dim3(p.blocks), dim3(1024), 0, st>>>(p);
-    route_place_kernel<<<dim3(p.blocks), dim3(1024), 0, st>>>(p);
+    route_choose_kernel<LPT, V, BIASED, false><<<dim3(p.blocks), dim3(waves * 64), route_lds_bytes(p, false), st>>>(p);
+    route_place_kernel<<<dim3(p.blocks), dim3(1024), route_lds_bytes(p, false), st>>>(p);
   }
+}
+template <int LPT, int V>
+void launch_route(const RouteParams& p, hipStream_t st) {
+  if (p.bias) launch_route_as<LPT, V, true>(p, st);
+  else launch_route_as<LPT, V, false>(p, st);
 }
 
 fupr_status check_router(const fupr_router& r) {
@@ -294,7 +307,14 @@ fupr_status check_router(const fupr_router& r) {
   return FUPR_OK;
 }
 
-int route_blocks(int T) { return (int)(((int64_t)T + kBlockTokens - 1) / kBlockTokens); }
+// How many times 64 tokens a workgroup takes.  The second launch reads a count per expert and workgroup in every
+// workgroup, so their number is held near one per compute unit; LDS holds a word per expert and 64 tokens.
+int route_groups(int T, int E) {
+  const int groups = (int)(((int64_t)T + 63) / 64);
+  if (T <= kOneTokens) return groups;
+  return std::max(1, std::min({(groups + kManyBlocks - 1) / kManyBlocks, 16, kWhoBytes / 8 / E}));
+}
+int route_blocks(int T, int E) { return (int)(((int64_t)T + route_groups(T, E) * 64 - 1) / (route_groups(T, E) * 64)); }
 
 // ---- weighted sum -----------------------------------------------------------
 
@@ -374,8 +394,8 @@ using namespace fupr;
 extern "C" {
 
 size_t fupr_moe_route_workspace_bytes(const fupr_router* router, int32_t tokens) {
-  if (!router || check_router(*router) != FUPR_OK || tokens <= kBlockTokens) return 0;
-  return (size_t)route_blocks(tokens) * (size_t)router->E * sizeof(int32_t);
+  if (!router || check_router(*router) != FUPR_OK || tokens <= kOneTokens) return 0;
+  return (size_t)route_blocks(tokens, router->E) * (size_t)router->E * sizeof(int32_t);
 }
 
 fupr_status fupr_moe_route(const fupr_router* router, const fupr_matrix* logits, int32_t* ids, float* weights,
@@ -388,7 +408,7 @@ fupr_status fupr_moe_route(const fupr_router* router, const fupr_matrix* logits,
   if (logits->rows > 0 && (!ids || !weights || !src || !pos)) return FUPR_ERR_NULL;
   for (const void* v : {(const void*)ids, (const void*)weights, (const void*)offsets, (const void*)src, (const void*)pos})
     if (reinterpret_cast<uintptr_t>(v) & 3) return FUPR_ERR_ALIGN;
-  if ((int64_t)logits->rows * router->top_k > 0x7fffffff - kBlockTokens * kMostChosen) return FUPR_ERR_LIMIT;
+  if ((int64_t)logits->rows * router->top_k > 0x7fffffff - 1024 * kMostChosen) return FUPR_ERR_LIMIT;
   const size_t needed = fupr_moe_route_workspace_bytes(router, logits->rows);
   if (needed > 0 && (!workspace || workspace_bytes < needed || (reinterpret_cast<uintptr_t>(workspace) & 255)))
     return FUPR_ERR_WORKSPACE;
@@ -411,14 +431,15 @@ fupr_status fupr_moe_route(const fupr_router* router, const fupr_matrix* logits,
   p.src = src;
   p.pos = pos;
   p.counts = (int32_t*)workspace;
-  p.blocks = route_blocks(p.T);
+  p.groups = route_groups(p.T, p.E);
+  p.blocks = route_blocks(p.T, p.E);
   hipStream_t s = (hipStream_t)stream;
   // the fewest lanes that hold a token's logits in 16 registers each, and one for every expert chosen
-  if (p.E <= 64 && p.k <= 8) launch_route_as<8, 8>(p, s);
-  else if (p.E <= 128 && p.k <= 8) launch_route_as<8, 16>(p, s);
-  else if (p.E <= 256) launch_route_as<16, 16>(p, s);
-  else if (p.E <= 512) launch_route_as<32, 16>(p, s);
-  else launch_route_as<64, 16>(p, s);
+  if (p.E <= 64 && p.k <= 8) launch_route<8, 8>(p, s);
+  else if (p.E <= 128 && p.k <= 8) launch_route<8, 16>(p, s);
+  else if (p.E <= 256) launch_route<16, 16>(p, s);
+  else if (p.E <= 512) launch_route<32, 16>(p, s);
+  else launch_route<64, 16>(p, s);
   return launch_status("route_choose_kernel");
 }
 
