@@ -3,8 +3,8 @@
 // of 128 bytes of every row of the tile goes global -> LDS as it lies (asynchronous loads of 16 bytes per lane that
 // need no registers), a ring of D buffers keeping D - 1 steps in flight.
 //
-// LDS row r holds its eight 16-byte chunks at chunk ^ (r & 7): the lanes of an operand read (16 rows, one chunk) then
-// fall on different banks.  Filters are MFMA operand A, rows of x operand B, so a lane ends up with four filters'
+// LDS row r holds its eight 16-byte chunks at chunk ^ (r / 2 & 7): the lanes of an operand read (16 rows, 128 bytes
+// apart, one chunk) then cover all 64 banks once.  Filters are MFMA operand A, rows of x operand B, so a lane ends up with four filters'
 // results of one row; which filter an LDS row holds is chosen such that a lane's tiles together are consecutive
 // columns of y (16-byte stores).  A gated layer alternates tiles of the gate and of the layer that it gates: both
 // results of a column meet in one lane.
@@ -137,9 +137,11 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
   const int n0 = nt * cols;
   const int steps = n0 < n_len ? (k_len + G::per_step - 1) / G::per_step : 0;
 
-  // the lane's place in every load: row lane / 8 of eight, chunk (lane & 7) ^ row
-  const int chunk = (lane & 7) ^ (lane >> 3);
-  const char* from[G::xl + G::wl];
+  // the lane's place in every load: row lane / 8 of eight, and the chunk that is kept there
+  static_assert(G::waves % 2 == 0, "the eight rows of a wave's loads are always even or always odd ones");
+  const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
+  constexpr int kLoads = G::xl + G::wl;
+  const char* from[kLoads];
 #pragma unroll
   for (int i = 0; i < G::xl; ++i) {
     int row = min(m0 + (i * G::waves + wave) * 8 + (lane >> 3), hi - 1);
@@ -157,17 +159,24 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
-  auto issue = [&](int step) {
-    const uint32_t to = lds0 + (step % D) * G::buf + wave * 1024;
-    // past the last chunk of a row (there are steps * 8 of them in the ring's eyes) the last one is read again: it
-    // lies inside the row, and what it brings is zeroed below
-    const int last = (k_len + G::per_chunk - 1) / G::per_chunk - 1;
-    const int back = max(step * 8 + chunk - last, 0) * 16;
-    const int64_t at = (int64_t)step * 128 - back;
+  // Loads of one step after the other into buffer after buffer.  In the step that the reduction ends in, chunks behind
+  // its last one are that last one again (inside the row, and zeroed below).
+  uint32_t to = lds0 + wave * 1024;
+  int issued = 0;
+  auto issue = [&]() {
+    if (++issued == steps) {
+      const int last = (k_len + G::per_chunk - 1) / G::per_chunk - 1;
+      const int back = max((steps - 1) * 8 + chunk - last, 0) * 16;
 #pragma unroll
-    for (int i = 0; i < G::xl; ++i) load_to_lds(from[i] + at, to + i * G::waves * 1024);
+      for (int i = 0; i < kLoads; ++i) from[i] -= back;
+    }
 #pragma unroll
-    for (int i = 0; i < G::wl; ++i) load_to_lds(from[G::xl + i] + at, to + BM * 128 + i * G::waves * 1024);
+    for (int i = 0; i < kLoads; ++i) {
+      load_to_lds(from[i], to + i * G::waves * 1024);
+      from[i] += 128;
+    }
+    to += G::buf;
+    if (to >= lds0 + D * G::buf) to -= D * G::buf;
   };
 
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -178,11 +187,11 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
     for (int j = 0; j < NT; ++j) acc[i][j] = zero;
 
   const int wm = wave / G::WN, wn = wave % G::WN;
-  const int row = (lane & 15) * 128, place = ((lane >> 4) ^ (lane & 7)) * 16;
-  constexpr int kLoads = G::xl + G::wl;
+  const int at0 = (lane & 15) * 128 + ((lane >> 4) ^ (lane >> 1 & 7)) * 16;
 #pragma unroll
   for (int s = 0; s < D - 1; ++s)
-    if (s < steps) issue(s);
+    if (s < steps) issue();
+  int buf = 0;
   for (int s = 0; s < steps; ++s) {
     if (s + D - 1 <= steps) wait_loads<(D - 2) * kLoads>();
     else wait_loads<0>();
@@ -191,7 +200,7 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
       // the last step of a reduction that does not fill it: zeros behind its end, in the wave's own part
       const int valid = left - chunk * G::per_chunk;
       if (valid < G::per_chunk) {
-        char* mine = lds + (s % D) * G::buf + wave * 1024 + lane * 16;
+        char* mine = lds + buf + wave * 1024 + lane * 16;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
           uint4* v = reinterpret_cast<uint4*>(mine + i * G::waves * 1024);
@@ -200,12 +209,12 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
       }
     }
     __syncthreads();
-    if (s + D - 1 < steps) issue(s + D - 1);
-    const char* xs = lds + (s % D) * G::buf + wm * MT * 2048;
-    const char* ws = lds + (s % D) * G::buf + BM * 128 + wn * NT * 2048;
+    if (s + D - 1 < steps) issue();
+    const char* xs = lds + buf + wm * MT * 2048;
+    const char* ws = lds + buf + BM * 128 + wn * NT * 2048;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const int at = row + (place ^ (half * 64));
+      const int at = at0 ^ (half * 64);
       uint4 a[NT], b[MT];
 #pragma unroll
       for (int j = 0; j < NT; ++j) a[j] = *reinterpret_cast<const uint4*>(ws + j * 2048 + at);
@@ -216,6 +225,7 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = mfma_chunks<G::TY>(a[j], b[i], acc[i][j]);
     }
+    buf = buf + G::buf == D * G::buf ? 0 : buf + G::buf;
   }
 
   const int row0 = m0 + wm * MT * 16;
@@ -242,7 +252,15 @@ fupr_status launch_as(LinearParams p, hipStream_t st) {
 
 template <int TY>
 fupr_status launch_type(const LinearParams& p, hipStream_t st) {
-  return launch_as<TileGeom<TY, 2, 2, 4, 4, 3>>(p, st);
+  switch (tuning_any() ? tuning_int("linear_tile", 0) : 0) {
+    case 1: return launch_as<TileGeom<TY, 2, 4, 8, 4, 2>>(p, st);
+    case 2: return launch_as<TileGeom<TY, 2, 4, 4, 4, 3>>(p, st);
+    case 3: return launch_as<TileGeom<TY, 2, 2, 2, 2, 4>>(p, st);
+    case 4: return launch_as<TileGeom<TY, 2, 2, 8, 8, 2>>(p, st);
+    case 5: return launch_as<TileGeom<TY, 2, 2, 4, 4, 2>>(p, st);
+    case 6: return launch_as<TileGeom<TY, 2, 2, 2, 4, 3>>(p, st);
+    default: return launch_as<TileGeom<TY, 2, 2, 4, 4, 3>>(p, st);
+  }
 }
 
 }  // namespace
