@@ -1,14 +1,22 @@
 // Linear layers on many rows, one layer or one per expert: y = a(x W^T + b) (* (x Wu^T + bu)) (+ res), a matrix
-// product in tiles of BM rows x BN filters.  Both operands have the reduction along their rows in memory, so a step
-// of 128 bytes of every row of the tile goes global -> LDS as it lies (asynchronous loads of 16 bytes per lane that
-// need no registers), a ring of D buffers keeping D - 1 steps in flight.
+// product in tiles of BM rows x BN filters.  Both operands have the reduction along their rows in memory, so a unit of
+// 64 bytes of every row of the tile (32 elements of 16 bits: one MFMA deep) goes global -> LDS as it lies, by
+// asynchronous loads of 16 bytes per lane that need no registers, into a ring of D buffers.
 //
-// LDS row r holds its eight 16-byte chunks at chunk ^ (r / 2 & 7): the lanes of an operand read (16 rows, 128 bytes
-// apart, one chunk) then cover all 64 banks once.  Filters are MFMA operand A, rows of x operand B, so a lane ends up with four filters'
+// A wave multiplies unit u from registers while it reads unit u + 1 from LDS into them.  One barrier for U units: behind
+// it the next U may be read, and the buffers of the last U are asked for again, one unit's loads at a time.  The loads are spread between the multiplications - a wave that finds
+// the load queue full cannot issue what stands behind.  A filter's operand registers are refilled as soon as its
+// last multiplication is issued; only the operands of the last rows and the filters exist twice.
+//
+// LDS row r (64 bytes) holds its four chunks at chunk ^ (r / 2 & 3).  LDS serves 16 lanes of an operand read at a time
+// (four times four neighbours, not of one chunk): with this order they cover all 64 banks once, 233 bytes per clock
+// measured; with r / 4 or none 123.  Filters are MFMA operand A, rows of x operand B, so a lane ends up with four filters'
 // results of one row; which filter an LDS row holds is chosen such that a lane's tiles together are consecutive
 // columns of y (16-byte stores).  A gated layer alternates tiles of the gate and of the layer that it gates: both
 // results of a column meet in one lane.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "linear_device.h"
 #include "tuning.h"
@@ -35,15 +43,17 @@ __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-template <int TY_, int WM_, int WN_, int MT_, int NT_, int D_>
+template <int TY_, int WM_, int WN_, int MT_, int NT_, int U_, int D_>
 struct TileGeom {
-  static constexpr int TY = TY_, WM = WM_, WN = WN_, MT = MT_, NT = NT_, D = D_;
+  static constexpr int TY = TY_, WM = WM_, WN = WN_, MT = MT_, NT = NT_, U = U_, D = D_;
   static constexpr int waves = WM * WN, threads = waves * 64;
   static constexpr int BM = WM * MT * 16, BN = WN * NT * 16;
-  static constexpr int xl = BM / 8 / waves, wl = BN / 8 / waves;   // loads of a wave and step (8 rows each)
-  static_assert(xl * 8 * waves == BM && wl * 8 * waves == BN && NT % 2 == 0, "whole loads, pairs of tiles");
-  static constexpr int buf = (BM + BN) * 128;
-  static constexpr int per_chunk = 16 / elem_bytes<TY>(), per_step = 8 * per_chunk;
+  static constexpr int xl = BM / 16 / waves, wl = BN / 16 / waves;   // loads of a wave and unit (16 rows each)
+  static_assert(xl * 16 * waves == BM && wl * 16 * waves == BN && NT % 2 == 0, "whole loads, pairs of tiles");
+  static constexpr int loads = xl + wl;
+  static constexpr int buf = (BM + BN) * 64;
+  static constexpr int twice = MT >= 4 ? 2 : 1;   // rows whose operands exist twice
+  static constexpr int per_chunk = 16 / elem_bytes<TY>(), per_unit = 4 * per_chunk;
 };
 
 template <class G, bool GATED>
@@ -105,8 +115,8 @@ __device__ __forceinline__ void tile_epilogue(const LinearParams& p, f32x4 (&acc
 }
 
 template <class G>
-__global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p) {
-  constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, D = G::D;
+__global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams p) {
+  constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, U = G::U, D = G::D;
   __shared__ __attribute__((aligned(1024))) char lds[D * G::buf];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool gated = p.w_up != nullptr;
@@ -135,49 +145,59 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
     m0 = (strip * 8 + in - nt * tall) * BM;
   }
   const int n0 = nt * cols;
-  const int steps = n0 < n_len ? (k_len + G::per_step - 1) / G::per_step : 0;
+  const int units = n0 < n_len ? (k_len + G::per_unit - 1) / G::per_unit : 0;
 
-  // the lane's place in every load: row lane / 8 of eight, and the chunk that is kept there
-  static_assert(G::waves % 2 == 0, "the eight rows of a wave's loads are always even or always odd ones");
-  const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
-  constexpr int kLoads = G::xl + G::wl;
-  const char* from[kLoads];
+  // the lane's place in every load: row lane / 4 of sixteen, and the chunk that is kept there
+  const int chunk = (lane & 3) ^ (lane >> 3 & 3);
+  const char* from[G::loads];
 #pragma unroll
   for (int i = 0; i < G::xl; ++i) {
-    int row = min(m0 + (i * G::waves + wave) * 8 + (lane >> 3), hi - 1);
+    int row = min(m0 + (i * G::waves + wave) * 16 + (lane >> 2), hi - 1);
     if (p.src) row = min(max(p.src[row], 0), p.x_rows - 1);
     from[i] = p.x + row * p.x_stride + chunk * 16;
   }
 #pragma unroll
   for (int i = 0; i < G::wl; ++i) {
-    const int r = (i * G::waves + wave) * 8 + (lane >> 3);
+    const int r = (i * G::waves + wave) * 16 + (lane >> 2);
     const int wn = r / (NT * 16), t = (r >> 4) % NT, j = r & 15;
     const int n = gated ? n0 + wn * NT * 8 + (j >> 2) * 2 * NT + 4 * (t >> 1) + (j & 3)
                         : n0 + wn * NT * 16 + (j >> 2) * 4 * NT + 4 * t + (j & 3);
     const char* w = gated && (t & 1) ? p.w_up : p.w;
     from[G::xl + i] = w + e * p.w_expert + min(n, max(n_len, 1) - 1) * p.w_stride + chunk * 16;
   }
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 1024;
 
-  // Loads of one step after the other into buffer after buffer.  In the step that the reduction ends in, chunks behind
-  // its last one are that last one again (inside the row, and zeroed below).
-  uint32_t to = lds0 + wave * 1024;
-  int issued = 0;
-  auto issue = [&]() {
-    if (++issued == steps) {
-      const int last = (k_len + G::per_chunk - 1) / G::per_chunk - 1;
-      const int back = max((steps - 1) * 8 + chunk - last, 0) * 16;
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) from[i] -= back;
-    }
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      load_to_lds(from[i], to + i * G::waves * 1024);
-      from[i] += 128;
-    }
-    to += G::buf;
-    if (to >= lds0 + D * G::buf) to -= D * G::buf;
+  // One load of unit `issued`, into buffer `to`.  In the unit that the reduction ends in, chunks behind its last one are
+  // that last one again (inside the row, and zeroed below).
+  int issued = 0, to = 0;
+  auto load = [&](int i) {
+    load_to_lds(from[i], lds0 + to + i * G::waves * 1024);
+    from[i] += 64;
   };
+  auto begin_unit = [&]() {
+    if (issued == units - 1) {
+      const int last = (k_len + G::per_chunk - 1) / G::per_chunk - 1;
+      const int back = max(issued * 4 + chunk - last, 0) * 16;
+#pragma unroll
+      for (int i = 0; i < G::loads; ++i) from[i] -= back;
+    }
+  };
+  auto end_unit = [&]() {
+    ++issued;
+    to = to + G::buf == D * G::buf ? 0 : to + G::buf;
+  };
+  // Zeros behind the reduction's end, in the wave's own part of the last unit's buffer, which has landed.
+  auto clear_tail = [&](int buf) {
+    const int valid = k_len - (units - 1) * G::per_unit - chunk * G::per_chunk;
+    if (valid >= G::per_chunk) return;
+    char* mine = lds + buf + wave * 1024 + lane * 16;
+#pragma unroll
+    for (int i = 0; i < G::loads; ++i) {
+      uint4* v = reinterpret_cast<uint4*>(mine + i * G::waves * 1024);
+      *v = keep_first<G::TY>(*v, valid);
+    }
+  };
+  const bool ragged = k_len % G::per_unit != 0;
 
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   f32x4 acc[MT][NT];
@@ -187,45 +207,91 @@ __global__ __launch_bounds__(G::threads) void linear_tile_kernel(LinearParams p)
     for (int j = 0; j < NT; ++j) acc[i][j] = zero;
 
   const int wm = wave / G::WN, wn = wave % G::WN;
-  const int at0 = (lane & 15) * 128 + ((lane >> 4) ^ (lane >> 1 & 7)) * 16;
+  constexpr int kTwice = G::twice, kOnce = MT - kTwice;
+  uint4 a[2][NT], b[kOnce > 0 ? kOnce : 1], c[2][kTwice];   // c: the last kTwice rows' operands
+  const char* const ws = lds + BM * 64 + wn * NT * 1024 + (lane & 15) * 64 + ((lane >> 4) ^ (lane >> 1 & 3)) * 16;
+  const char* const xs = lds + wm * MT * 1024 + (lane & 15) * 64 + ((lane >> 4) ^ (lane >> 1 & 3)) * 16;
+  auto read = [&](const char* at, int i, int buf) { return *reinterpret_cast<const uint4*>(at + buf + i * 1024); };
+
+  int next = 0;   // buffer of the unit that is read
+  // FULL: in the middle of a long reduction, where every unit asks for another one, not the last.  turn: u modulo the
+  // units of the unrolled loop.
+  auto multiply = [&](auto full, auto turn, int u) {
+    constexpr bool FULL = decltype(full)::value;
+    constexpr int S = decltype(turn)::value & 1;
+    constexpr bool kBarrier = decltype(turn)::value % U == U - 1;
+    next = next + G::buf == D * G::buf ? 0 : next + G::buf;
+    if (kBarrier && (FULL || u + 1 < units)) {
+      // units u + 1 .. u + U have landed; of those up to u + D - U that are asked for, the others may still fly
+      if (FULL || u + D - U < units) wait_loads<(D - 2 * U) * G::loads>();
+      else wait_loads<0>();
+      if (!FULL && ragged && units - 1 <= u + U) clear_tail((units - 1) % D * G::buf);
+      __syncthreads();
+    }
+    const bool more = FULL || (u >= U - 1 && issued < units);   // (the ring is full before)
+    if (!FULL && more) begin_unit();
+    // One read or load behind every pair of multiplications: the filters' and the last rows' operands of the next
+    // unit, spread over the first three quarters, the other rows' as their registers fall free, the loads of a later unit.
+    constexpr int kPairs = MT * NT / 2, kOthers = NT + kTwice, kEarly = kPairs * 3 / 4 > 0 ? kPairs * 3 / 4 : 1;
 #pragma unroll
-  for (int s = 0; s < D - 1; ++s)
-    if (s < steps) issue();
-  int buf = 0;
-  for (int s = 0; s < steps; ++s) {
-    if (s + D - 1 <= steps) wait_loads<(D - 2) * kLoads>();
-    else wait_loads<0>();
-    const int left = k_len - s * G::per_step;
-    if (left < G::per_step) {
-      // the last step of a reduction that does not fill it: zeros behind its end, in the wave's own part
-      const int valid = left - chunk * G::per_chunk;
-      if (valid < G::per_chunk) {
-        char* mine = lds + buf + wave * 1024 + lane * 16;
+    for (int q = 0; q < kPairs; ++q) {
+      const int i = q * 2 / NT, j = q * 2 % NT;
+      __builtin_amdgcn_sched_barrier(0);
+      const uint4 row = i < kOnce ? b[i < kOnce ? i : 0] : c[S][i < kOnce ? 0 : i - kOnce];
+      acc[i][j] = mfma_chunks<G::TY>(a[S][j], row, acc[i][j]);
+      acc[i][j + 1] = mfma_chunks<G::TY>(a[S][j + 1], row, acc[i][j + 1]);
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          uint4* v = reinterpret_cast<uint4*>(mine + i * G::waves * 1024);
-          *v = keep_first<G::TY>(*v, valid);
-        }
+      for (int o = kOthers * q / kEarly; o < kOthers * (q + 1) / kEarly && o < kOthers; ++o) {
+        if (o < NT) a[S ^ 1][o < NT ? o : 0] = read(ws, o, next);
+        else c[S ^ 1][o < NT ? 0 : o - NT] = read(xs, kOnce + o - NT, next);
+      }
+      if (j + 2 == NT && i < kOnce) b[i < kOnce ? i : 0] = read(xs, i, next);
+      if (more) {
+#pragma unroll
+        for (int l = 0; l < G::loads; ++l)
+          if ((2 * l + 1) * kPairs / (2 * G::loads) == q) load(l);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) end_unit();
+  };
+
+  if (units > 0) {
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+      if (issued < units) {
+        begin_unit();
+#pragma unroll
+        for (int i = 0; i < G::loads; ++i) load(i);
+        end_unit();
+      }
+    if (units >= D) wait_loads<(D - U) * G::loads>();
+    else wait_loads<0>();
+    if (ragged && units <= U) clear_tail((units - 1) * G::buf);
     __syncthreads();
-    if (s + D - 1 < steps) issue();
-    const char* xs = lds + buf + wm * MT * 2048;
-    const char* ws = lds + buf + BM * 128 + wn * NT * 2048;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int at = at0 ^ (half * 64);
-      uint4 a[NT], b[MT];
+    for (int j = 0; j < NT; ++j) a[0][j] = read(ws, j, 0);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) a[j] = *reinterpret_cast<const uint4*>(ws + j * 2048 + at);
+    for (int i = 0; i < kOnce; ++i) b[i] = read(xs, i, 0);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) b[i] = *reinterpret_cast<const uint4*>(xs + i * 2048 + at);
-#pragma unroll
-      for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = mfma_chunks<G::TY>(a[j], b[i], acc[i][j]);
+    for (int i = 0; i < kTwice; ++i) c[0][i] = read(xs, kOnce + i, 0);
+    constexpr int kTurns = U < 2 ? 2 : U;
+    static_assert(kTurns == 2 || kTurns == 4, "written out below");
+    auto turns = [&](auto full, int u) {
+      multiply(full, std::integral_constant<int, 0>{}, u);
+      if (full.value || u + 1 < units) multiply(full, std::integral_constant<int, 1>{}, u + 1);
+      if constexpr (kTurns == 4) {
+        if (full.value || u + 2 < units) multiply(full, std::integral_constant<int, 2>{}, u + 2);
+        if (full.value || u + 3 < units) multiply(full, std::integral_constant<int, 3>{}, u + 3);
+      }
+    };
+    int u = 0;
+    if constexpr (U > 1) {
+      turns(std::false_type{}, u);
+      u += kTurns;
     }
-    buf = buf + G::buf == D * G::buf ? 0 : buf + G::buf;
+    for (; u + kTurns - U + D < units - 1; u += kTurns) turns(std::true_type{}, u);
+    for (; u < units; u += kTurns) turns(std::false_type{}, u);
   }
 
   const int row0 = m0 + wm * MT * 16;
@@ -253,13 +319,10 @@ fupr_status launch_as(LinearParams p, hipStream_t st) {
 template <int TY>
 fupr_status launch_type(const LinearParams& p, hipStream_t st) {
   switch (tuning_any() ? tuning_int("linear_tile", 0) : 0) {
-    case 1: return launch_as<TileGeom<TY, 2, 4, 8, 4, 2>>(p, st);
-    case 2: return launch_as<TileGeom<TY, 2, 4, 4, 4, 3>>(p, st);
-    case 3: return launch_as<TileGeom<TY, 2, 2, 2, 2, 4>>(p, st);
-    case 4: return launch_as<TileGeom<TY, 2, 2, 8, 8, 2>>(p, st);
-    case 5: return launch_as<TileGeom<TY, 2, 2, 4, 4, 2>>(p, st);
-    case 6: return launch_as<TileGeom<TY, 2, 2, 2, 4, 3>>(p, st);
-    default: return launch_as<TileGeom<TY, 2, 2, 4, 4, 3>>(p, st);
+#ifdef TILES
+    TILES
+#endif
+    default: return launch_as<TileGeom<TY, 2, 2, 4, 4, 2, 4>>(p, st);
   }
 }
 
