@@ -30,6 +30,10 @@ struct LinearParams {
 // linear_tile.hip: tiles of rows and filters staged through LDS.
 fupr_status launch_linear_tile(LinearParams p, fupr_dtype dt, void* stream);
 
+// linear_wide.hip: tiles of 256 x 256, 16-bit types.  linear_wide_applies: of these types and strides.
+bool linear_wide_applies(const LinearParams& p, fupr_dtype dt);
+fupr_status launch_linear_wide(LinearParams p, fupr_dtype dt, void* stream);
+
 // linear_rows.hip: few rows, bound by reading the weights once.  linear_rows_applies: of these sizes and strides.
 bool linear_rows_applies(const LinearParams& p, fupr_dtype dt);
 fupr_status launch_linear_rows(LinearParams p, fupr_dtype dt, void* stream);

@@ -1,0 +1,189 @@
+// Internal: what the kernels of linear layers on many rows share - where a workgroup's tile lies, which filter an LDS
+// row holds, loads into LDS, the epilogue from accumulators.
+#pragma once
+#include "linear_device.h"
+
+namespace fupr {
+
+// 64 lanes x 16 bytes from their own addresses to 1024 consecutive bytes of LDS
+__device__ __forceinline__ void load_to_lds(const char* from, uint32_t lds_base) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, off"
+      :
+      : "s"(lds_base), "v"(from)
+      : "memory", "m0");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Where a workgroup's tile lies: rows m0 .. of those below hi, column tile nt, of expert e.
+struct TilePlace {
+  int e, hi, m0, nt, n_len, k_len;
+};
+template <int BM>
+__device__ __forceinline__ bool find_tile(const LinearParams& p, int lane, TilePlace& t) {
+  if (p.offsets) {
+    const int at = tile_of_workgroup(blockIdx.x, count_expert_tiles<BM>(p, lane) * p.n_tiles);
+    if (at < 0) return false;
+    ExpertRows r;
+    const int mt = at / p.n_tiles;
+    if (!find_expert<BM>(p, mt, lane, r)) return false;
+    t = TilePlace{r.e, r.hi, r.lo + r.tile * BM, at - mt * p.n_tiles, r.n_len, r.k_len};
+    return true;
+  }
+  // strips of eight row tiles: what an XCD holds at one time is about as tall as it is wide
+  const int at = tile_of_workgroup(blockIdx.x, p.m_tiles * p.n_tiles);
+  if (at < 0) return false;
+  const int strip = at / (8 * p.n_tiles), tall = min(8, p.m_tiles - strip * 8);
+  const int in = at - strip * 8 * p.n_tiles, nt = in / tall;
+  t = TilePlace{0, p.M, (strip * 8 + in - nt * tall) * BM, nt, p.N, p.K};
+  return true;
+}
+
+// Which column of the tile the filter in LDS row r belongs to, for waves of NT tiles of 16 filters.  MFMA leaves a
+// lane of group g = lane / 16 with filters 4 g .. 4 g + 3 of each of its tiles; here the tiles of a lane follow each
+// other.  Gated: odd tiles hold the gated layer's filters of the same columns.
+template <int NT>
+__device__ __forceinline__ int filter_of(int r, bool gated) {
+  const int wn = r / (NT * 16), t = (r >> 4) % NT, j = r & 15;
+  return gated ? wn * NT * 8 + (j >> 2) * 2 * NT + 4 * (t >> 1) + (j & 3)
+               : wn * NT * 16 + (j >> 2) * 4 * NT + 4 * t + (j & 3);
+}
+
+// The results of one row from column n on, 16 bytes of them at 16 bits: what is added to them, in its own type.
+template <int TY>
+struct Addend {
+  uint4 v[2];
+};
+template <int TY>
+__device__ __forceinline__ Addend<TY> load_addend(const LinearParams& p, int64_t row, int n, bool there) {
+  Addend<TY> a;
+  a.v[0] = a.v[1] = uint4{0u, 0u, 0u, 0u};
+  if (there && p.res && n < p.N) {
+    const bool f32 = TY == FUPR_F32 || p.y_f32;
+    // (pieces of 16 bytes lie inside the row's memory, which ends at a multiple of 16)
+    const char* r = p.res + row * p.res_stride + (int64_t)n * (f32 ? 4 : 2);
+    a.v[0] = *reinterpret_cast<const uint4*>(r);
+    if (f32 && n + 4 < p.N) a.v[1] = *reinterpret_cast<const uint4*>(r + 16);
+  }
+  return a;
+}
+template <int TY>
+__device__ __forceinline__ void store_row(const LinearParams& p, int64_t row, int n, float (&v)[8], const Addend<TY>& add) {
+  const bool whole = n + 8 <= p.N;
+  const uint32_t d[8] = {add.v[0].x, add.v[0].y, add.v[0].z, add.v[0].w, add.v[1].x, add.v[1].y, add.v[1].z, add.v[1].w};
+  if (TY == FUPR_F32 || p.y_f32) {
+    float* y = reinterpret_cast<float*>(p.y + row * p.y_stride) + n;
+    if (p.res) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(d[i]);
+    }
+    if (whole) {
+      *reinterpret_cast<f32x4*>(y) = f32x4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4*>(y + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (n + i < p.N) y[i] = v[i];
+    }
+  } else {
+    constexpr bool BF = TY == FUPR_BF16;
+    uint16_t* y = reinterpret_cast<uint16_t*>(p.y + row * p.y_stride) + n;
+    if (p.res) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += to_float<BF>((uint16_t)(d[i / 2] >> (i & 1) * 16));
+    }
+    if (whole) {
+      *reinterpret_cast<uint4*>(y) = uint4{pack2<BF>(v[0], v[1]), pack2<BF>(v[2], v[3]), pack2<BF>(v[4], v[5]), pack2<BF>(v[6], v[7])};
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (n + i < p.N) y[i] = from_float<BF>(v[i]);
+    }
+  }
+}
+
+// From a wave's accumulators to y.  They pass through the wave's own part of LDS, EM row tiles at a time, so that eight
+// consecutive columns of a row meet in a lane and the rest is a loop that is not written out for every register: a
+// version straight from the registers spilled them and took 10 us more for a tile of 256 x 256.  LDS rows of NT * 4
+// chunks of four columns (gated: the gate's half, then the other's) hold chunk c at c ^ (row modulo their number).
+// nb: the wave's first column.
+template <int TY, int MT, int NT, int EM, bool GATED>
+__device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4 (&acc)[MT][NT], char* lds, int e, int hi,
+                                              int row0, int nb, int n_len, int lane) {
+  constexpr bool FINE = TY == FUPR_F32;
+  constexpr int kChunks = NT * 4, kCols = GATED ? NT * 8 : NT * 16;   // of a row
+  constexpr int kLanes = kCols / 8, kRows = 64 / kLanes, kTurns = EM * 16 / kRows;
+  static_assert(MT % EM == 0, "whole parts");
+  const int c = lane % kLanes, n = nb + c * 8;
+  float bias[8], up[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    bias[i] = p.bias && n + i < n_len ? p.bias[(int64_t)e * p.N + n + i] : 0.f;
+    up[i] = GATED && p.bias_up && n + i < n_len ? p.bias_up[(int64_t)e * p.N + n + i] : 0.f;
+  }
+#pragma unroll
+  for (int part = 0; part < MT / EM; ++part) {
+    const int first = row0 + part * EM * 16 + lane / kLanes;
+#pragma unroll
+    for (int i = 0; i < EM; ++i)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const int r = lane & 15, g = lane >> 4;
+        const int at = GATED ? (t & 1) * (kChunks / 2) + g * (NT / 2) + t / 2 : g * NT + t;
+        *reinterpret_cast<f32x4*>(lds + (i * 16 + r) * kChunks * 16 + ((at ^ r) & (kChunks - 1)) * 16) = acc[part * EM + i][t];
+      }
+#pragma unroll 1
+    for (int turn = 0; turn < kTurns; ++turn) {
+      const int r = turn * kRows + lane / kLanes, row = first + turn * kRows;
+      const char* from = lds + r * kChunks * 16;
+      float v[8], u[8];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(from + (((c * 2 + q) ^ r) & (kChunks - 1)) * 16);
+        f32x4 b = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (GATED) b = *reinterpret_cast<const f32x4*>(from + (((kChunks / 2 + c * 2 + q) ^ r) & (kChunks - 1)) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[q * 4 + i] = a[i] + bias[q * 4 + i];
+          u[q * 4 + i] = b[i] + up[q * 4 + i];
+        }
+      }
+      const Addend<TY> add = load_addend<TY>(p, row, n, row < hi);
+      with_activation(p.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = activate<FINE, decltype(act)::value>(v[i]);
+      });
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (GATED) v[i] *= u[i];
+        if (n + i >= n_len) v[i] = 0.f;   // columns that pruning took from this expert
+      }
+      if (row < hi && n < p.N) store_row<TY>(p, row, n, v, add);
+    }
+  }
+}
+
+// Tiles of a launch, as a multiple of eight (workgroups go to the eight XCDs in turn); false: more than a grid holds.
+inline bool count_tiles(LinearParams& p, int BM, int BN, unsigned* blocks) {
+  const int cols = p.w_up ? BN / 2 : BN;
+  p.n_tiles = (p.N + cols - 1) / cols;
+  if (p.offsets) {
+    // at most: one tile begun by every expert that can have a row, the others full
+    const int begun = p.E < p.M ? p.E : p.M;
+    p.m_tiles = begun + (p.M - begun) / BM;
+  } else {
+    p.m_tiles = (p.M + BM - 1) / BM;
+  }
+  const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
+  if (tiles > 0x7fffff00) return false;
+  *blocks = (unsigned)((tiles + 7) / 8 * 8);
+  return true;
+}
+
+}  // namespace fupr

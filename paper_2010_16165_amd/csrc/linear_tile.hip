@@ -18,7 +18,7 @@
 
 #include <type_traits>
 
-#include "linear_device.h"
+#include "linear_tile.h"
 #include "tuning.h"
 
 namespace fupr {
@@ -26,22 +26,6 @@ namespace fupr {
 fupr_status launch_status(const char* what);
 
 namespace {
-
-// 64 lanes x 16 bytes from their own addresses to 1024 consecutive bytes of LDS
-__device__ __forceinline__ void load_to_lds(const char* from, uint32_t lds_base) {
-  asm volatile(
-      "s_mov_b32 m0, %0\n\t"
-      "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %1, off"
-      :
-      : "s"(lds_base), "v"(from)
-      : "memory", "m0");
-}
-
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
 
 template <int TY_, int WM_, int WN_, int MT_, int NT_, int U_, int D_>
 struct TileGeom {
@@ -56,64 +40,6 @@ struct TileGeom {
   static constexpr int per_chunk = 16 / elem_bytes<TY>(), per_unit = 4 * per_chunk;
 };
 
-template <class G, bool GATED>
-__device__ __forceinline__ void tile_epilogue(const LinearParams& p, f32x4 (&acc)[G::MT][G::NT], int e, int hi, int row0,
-                                              int nb, int n_len, int lane) {
-  constexpr int NT = G::NT, MT = G::MT, Q = GATED ? NT / 2 : NT;   // four-column pieces of a lane
-  constexpr bool FINE = G::TY == FUPR_F32;
-  const int n0 = nb + (lane >> 4) * 4 * Q;
-  const float* b = p.bias ? p.bias + (int64_t)e * p.N : nullptr;
-  const float* bu = p.bias_up ? p.bias_up + (int64_t)e * p.N : nullptr;
-  auto add = [&](const float* from, int first, int step) {
-    if (!from) return;
-#pragma unroll
-    for (int q = 0; q < Q; ++q)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int n = n0 + q * 4 + i;
-        const float v = n < n_len ? from[n] : 0.f;
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) acc[mt][first + q * step][i] += v;
-      }
-  };
-  add(b, 0, GATED ? 2 : 1);
-  if constexpr (GATED) add(bu, 1, 2);
-  with_activation(p.act, [&](auto act) {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int q = 0; q < Q; ++q)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float v = activate<FINE, decltype(act)::value>(acc[mt][GATED ? 2 * q : q][i]);
-          if constexpr (GATED) v *= acc[mt][2 * q + 1][i];
-          acc[mt][GATED ? 2 * q : q][i] = v;
-        }
-  });
-  if (nb + 4 * Q * 4 > n_len) {   // columns that pruning took from this expert
-#pragma unroll
-    for (int q = 0; q < Q; ++q)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (n0 + q * 4 + i >= n_len)
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) acc[mt][GATED ? 2 * q : q][i] = 0.f;
-  }
-  constexpr int kPer = Q % 2 ? 1 : 2;
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt) {
-    const int row = row0 + mt * 16 + (lane & 15);
-    if (row >= hi) continue;
-#pragma unroll
-    for (int q = 0; q < Q; q += kPer) {
-      float v[4 * kPer];
-#pragma unroll
-      for (int i = 0; i < 4 * kPer; ++i) v[i] = acc[mt][GATED ? 2 * (q + i / 4) : q + i / 4][i & 3];
-      store_run<G::TY, 4 * kPer>(p, row, n0 + q * 4, v);
-    }
-  }
-}
-
 template <class G>
 __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams p) {
   constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, U = G::U, D = G::D;
@@ -122,29 +48,10 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
   const bool gated = p.w_up != nullptr;
   const int cols = gated ? BN / 2 : BN;   // of y, in a tile
 
-  int e = 0, hi = p.M, m0, nt, n_len = p.N, k_len = p.K;
-  if (p.offsets) {
-    const int at = tile_of_workgroup(blockIdx.x, count_expert_tiles<BM>(p, lane) * p.n_tiles);
-    if (at < 0) return;
-    ExpertRows r;
-    const int mt = at / p.n_tiles;
-    nt = at - mt * p.n_tiles;
-    if (!find_expert<BM>(p, mt, lane, r)) return;
-    e = r.e;
-    hi = r.hi;
-    m0 = r.lo + r.tile * BM;
-    n_len = r.n_len;
-    k_len = r.k_len;
-  } else {
-    // strips of eight row tiles: what an XCD holds at one time is about as tall as it is wide
-    const int at = tile_of_workgroup(blockIdx.x, p.m_tiles * p.n_tiles);
-    if (at < 0) return;
-    const int strip = at / (8 * p.n_tiles), tall = min(8, p.m_tiles - strip * 8);
-    const int in = at - strip * 8 * p.n_tiles;
-    nt = in / tall;
-    m0 = (strip * 8 + in - nt * tall) * BM;
-  }
-  const int n0 = nt * cols;
+  TilePlace at;
+  if (!find_tile<BM>(p, lane, at)) return;
+  const int e = at.e, hi = at.hi, m0 = at.m0, n_len = at.n_len, k_len = at.k_len;
+  const int n0 = at.nt * cols;
   const int units = n0 < n_len ? (k_len + G::per_unit - 1) / G::per_unit : 0;
 
   // the lane's place in every load: row lane / 4 of sixteen, and the chunk that is kept there
@@ -159,11 +66,8 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
 #pragma unroll
   for (int i = 0; i < G::wl; ++i) {
     const int r = (i * G::waves + wave) * 16 + (lane >> 2);
-    const int wn = r / (NT * 16), t = (r >> 4) % NT, j = r & 15;
-    const int n = gated ? n0 + wn * NT * 8 + (j >> 2) * 2 * NT + 4 * (t >> 1) + (j & 3)
-                        : n0 + wn * NT * 16 + (j >> 2) * 4 * NT + 4 * t + (j & 3);
-    const char* w = gated && (t & 1) ? p.w_up : p.w;
-    from[G::xl + i] = w + e * p.w_expert + min(n, max(n_len, 1) - 1) * p.w_stride + chunk * 16;
+    const char* w = gated && (r >> 4 & 1) ? p.w_up : p.w;
+    from[G::xl + i] = w + e * p.w_expert + min(n0 + filter_of<NT>(r, gated), max(n_len, 1) - 1) * p.w_stride + chunk * 16;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 1024;
 
@@ -191,7 +95,7 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
     const int valid = k_len - (units - 1) * G::per_unit - chunk * G::per_chunk;
     if (valid >= G::per_chunk) return;
     char* mine = lds + buf + wave * 1024 + lane * 16;
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < G::loads; ++i) {
       uint4* v = reinterpret_cast<uint4*>(mine + i * G::waves * 1024);
       *v = keep_first<G::TY>(*v, valid);
@@ -214,8 +118,8 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
   auto read = [&](const char* at, int i, int buf) { return *reinterpret_cast<const uint4*>(at + buf + i * 1024); };
 
   int next = 0;   // buffer of the unit that is read
-  // FULL: in the middle of a long reduction, where every unit asks for another one, not the last.  turn: u modulo the
-  // units of the unrolled loop.
+  // FULL: in the middle of a long reduction, where every unit asks for another one, not the last: no branches between
+  // the multiplications.  turn: u modulo the units of the unrolled loop.
   auto multiply = [&](auto full, auto turn, int u) {
     constexpr bool FULL = decltype(full)::value;
     constexpr int S = decltype(turn)::value & 1;
@@ -295,24 +199,19 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
   }
 
   const int row0 = m0 + wm * MT * 16;
-  if (gated) tile_epilogue<G, true>(p, acc, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
-  else tile_epilogue<G, false>(p, acc, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
+  __syncthreads();   // (no wave reads operands any more)
+  constexpr int kMine = 16 * NT * 64;   // bytes of a row tile of accumulators
+  constexpr int EM = G::waves * MT * kMine <= D * G::buf ? MT : G::waves * MT * kMine <= 2 * D * G::buf ? MT / 2 : MT / 4;
+  char* mine = lds + wave * EM * kMine;
+  if (gated) tile_epilogue<G::TY, MT, NT, EM, true>(p, acc, mine, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
+  else tile_epilogue<G::TY, MT, NT, EM, false>(p, acc, mine, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
 }
 
 template <class G>
 fupr_status launch_as(LinearParams p, hipStream_t st) {
-  const int cols = p.w_up ? G::BN / 2 : G::BN;
-  p.n_tiles = (p.N + cols - 1) / cols;
-  if (p.offsets) {
-    // at most: one tile begun by every expert that can have a row, the others full
-    const int begun = p.E < p.M ? p.E : p.M;
-    p.m_tiles = begun + (p.M - begun) / G::BM;
-  } else {
-    p.m_tiles = (p.M + G::BM - 1) / G::BM;
-  }
-  const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
-  if (tiles > 0x7fffff00) return FUPR_ERR_LIMIT;
-  linear_tile_kernel<G><<<dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(G::threads), 0, st>>>(p);
+  unsigned blocks;
+  if (!count_tiles(p, G::BM, G::BN, &blocks)) return FUPR_ERR_LIMIT;
+  linear_tile_kernel<G><<<dim3(blocks), dim3(G::threads), 0, st>>>(p);
   return launch_status("linear_tile_kernel");
 }
 
@@ -329,6 +228,7 @@ fupr_status launch_type(const LinearParams& p, hipStream_t st) {
 }  // namespace
 
 fupr_status launch_linear_tile(LinearParams p, fupr_dtype dt, void* stream) {
+  if (tuning_any() && tuning_int("linear_tile", 0) == 99 && linear_wide_applies(p, dt)) return launch_linear_wide(p, dt, stream);
   hipStream_t st = (hipStream_t)stream;
   switch (dt) {
     case FUPR_BF16: return launch_type<FUPR_BF16>(p, st);
