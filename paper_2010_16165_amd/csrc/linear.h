@@ -30,9 +30,9 @@ struct LinearParams {
 // linear_tile.hip: tiles of rows and filters staged through LDS.
 fupr_status launch_linear_tile(LinearParams p, fupr_dtype dt, void* stream);
 
-// linear_wide.hip: tiles of 256 x 256, 16-bit types.  linear_wide_applies: of these types and strides.
+// linear_wide.hip: tiles of 256 or 128 rows x 256 filters, 16-bit types.  linear_wide_applies: of these types and strides.
 bool linear_wide_applies(const LinearParams& p, fupr_dtype dt);
-fupr_status launch_linear_wide(LinearParams p, fupr_dtype dt, void* stream);
+fupr_status launch_linear_wide(LinearParams p, fupr_dtype dt, int rows, void* stream);
 
 // linear_rows.hip: few rows, bound by reading the weights once.  linear_rows_applies: of these sizes and strides.
 bool linear_rows_applies(const LinearParams& p, fupr_dtype dt);

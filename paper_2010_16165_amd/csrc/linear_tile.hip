@@ -228,7 +228,8 @@ fupr_status launch_type(const LinearParams& p, hipStream_t st) {
 }  // namespace
 
 fupr_status launch_linear_tile(LinearParams p, fupr_dtype dt, void* stream) {
-  if (tuning_any() && tuning_int("linear_tile", 0) == 99 && linear_wide_applies(p, dt)) return launch_linear_wide(p, dt, stream);
+  const int forced = tuning_any() ? tuning_int("linear_tile", 0) : 0;
+  if ((forced == 99 || forced == 98) && linear_wide_applies(p, dt)) return launch_linear_wide(p, dt, forced == 99 ? 256 : 128, stream);
   hipStream_t st = (hipStream_t)stream;
   switch (dt) {
     case FUPR_BF16: return launch_type<FUPR_BF16>(p, st);

@@ -1,14 +1,14 @@
-// Linear layers on very many rows, 16-bit types: tiles of 256 rows x 256 filters on eight waves of 128 x 64.
+// Linear layers on very many rows, 16-bit types: tiles of 256 or 128 rows x 256 filters on eight waves.
 //
 // Why so large: a compute unit takes in 64 bytes per clock, and 128 x 128 tiles need that much to keep the matrix
-// units busy; these need half.  A step of 128 bytes of every row (64 elements, whole lines) goes global -> LDS as in
-// linear_tile.hip, two buffers of 64 KB.
+// units busy; these need half and three quarters of it.  A step of 128 bytes of every row (64 elements, whole lines)
+// goes global -> LDS as in linear_tile.hip, into D buffers.
 //
 // The waves' halves take turns: while the first four (one per SIMD) multiply a step from registers, the other four
-// read theirs from LDS, all of it, 96 registers beside 128 of accumulators.  Each phase ends in a barrier; in it one
-// half does nothing but multiply, at a raised wave priority.  Phase 2 s: the first half reads step s, the second
-// multiplies s - 1, and both ask for step s + 1 into the buffer that the second half has read to its end in phase
-// 2 s - 1; it has landed when phase 2 s + 1 ends.
+// read theirs from LDS, all of it (at 256 rows 96 registers beside 128 of accumulators).  Each phase ends in a barrier;
+// in it one half does nothing but multiply, at a raised wave priority.  Phase 2 s: the first half reads step s, the
+// second multiplies s - 1, and both ask for step s + D - 1 into the buffer that the second half has read to its end in
+// phase 2 s - 1.
 //
 // LDS row r (128 bytes) holds its eight chunks at chunk ^ (r / 2 & 7): operand reads cover all 64 banks once.
 #include <hip/hip_runtime.h>
@@ -23,8 +23,7 @@ fupr_status launch_status(const char* what);
 
 namespace {
 
-constexpr int BM = 256, BN = 256, MT = 8, NT = 4, kWaves = 8, kLoads = 8;   // loads: of a wave and step, 8 rows each
-constexpr int kBuf = (BM + BN) * 128;
+constexpr int BN = 256, NT = 4, kWaves = 8;
 
 // The end of a phase: what this wave read from LDS has arrived, and no wave goes on before all have come here.
 __device__ __forceinline__ void phase_ends() {
@@ -44,15 +43,11 @@ __device__ __forceinline__ void load_to_lds_from(const char* base, uint32_t off,
       : "memory", "m0");
 }
 
-__device__ __forceinline__ uint4 read_lds(uint32_t at) {
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  return __builtin_bit_cast(uint4, *(const u32x4 __attribute__((address_space(3)))*)(uintptr_t)at);
-}
-
-template <int TY>
+template <int TY, int MT, int D>
 __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParams p) {
   constexpr int kChunk = 8, kStep = 64;   // elements
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kBuf];
+  constexpr int BM = 32 * MT, XL = BM / 64, kLoads = XL + 4, kBuf = (BM + BN) * 128;   // loads: 8 rows each, of a wave
+  __shared__ __attribute__((aligned(1024))) char lds[D * kBuf];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const bool gated = p.w_up != nullptr;
   TilePlace at;
@@ -68,7 +63,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
   const char* wb = p.w + e * p.w_expert + n0 * p.w_stride;
   const char* ub = gated ? p.w_up + e * p.w_expert + n0 * p.w_stride : wb;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < XL; ++i) {
     const int row = min(m0 + (i * kWaves + wave) * 8 + (lane >> 3), hi - 1);
     const int from = p.src ? min(max(p.src[row], 0), p.x_rows - 1) : row - m0;
     off[i] = (uint32_t)from * (uint32_t)p.x_stride + chunk * 16;
@@ -76,7 +71,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int n = min(filter_of<NT>((i * kWaves + wave) * 8 + (lane >> 3), gated), max(n_len - n0, 1) - 1);
-    off[4 + i] = (uint32_t)n * (uint32_t)p.w_stride + chunk * 16;
+    off[XL + i] = (uint32_t)n * (uint32_t)p.w_stride + chunk * 16;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 1024;
   // LDS rows of load i: (i * 8 + wave) * 8 ..; an odd tile of 16 is the gated layer's
@@ -88,7 +83,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
   int issued = 0;
   uint32_t to = 0;
   auto load = [&](int i) {
-    load_to_lds_from(i < 4 ? xb : fb, off[i], lds0 + to + i * kWaves * 1024);
+    load_to_lds_from(i < XL ? xb : fb, off[i], lds0 + to + i * kWaves * 1024);
   };
   auto begin_step = [&]() {
     if (issued == steps - 1) {
@@ -102,7 +97,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
     ++issued;
     xb += 128;
     fb += 128;
-    to ^= kBuf;
+    to = to + kBuf == D * kBuf ? 0 : to + kBuf;
   };
   auto issue = [&]() {
     begin_step();
@@ -110,13 +105,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
     for (int i = 0; i < kLoads; ++i) load(i);
     end_step();
   };
-  // Step s has landed; zeros behind the reduction's end, in the wave's own part of it.
+  // Step s has landed, with D - 2 later ones still in flight; zeros behind the reduction's end, in the wave's own part.
   auto landed = [&](int s) {
     if (s >= steps) return;
-    wait_loads<0>();
+    if (D > 2 && s + D - 2 < steps) wait_loads<(D - 2) * kLoads>();
+    else wait_loads<0>();
     const int valid = k_len - s * kStep - chunk * kChunk;
     if (s == steps - 1 && valid < kChunk) {
-      char* mine = lds + (s & 1) * kBuf + wave * 1024 + lane * 16;
+      char* mine = lds + s % D * kBuf + wave * 1024 + lane * 16;
 #pragma unroll 1
       for (int i = 0; i < kLoads; ++i) {
         uint4* v = reinterpret_cast<uint4*>(mine + i * kWaves * 1024);
@@ -133,24 +129,22 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
     for (int j = 0; j < NT; ++j) acc[i][j] = zero;
   const int wm = wave / 4, wn = wave % 4;
   uint4 a[2][NT], b[2][MT];   // of the two halves of a step
-  // LDS addresses of the wave's operands in the two halves of the step that is read next (the kernel's only shared
-  // array starts at address 0, its second buffer at bit 16)
-  const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds +
-                         (lane & 15) * 128 + ((lane >> 4) ^ (lane >> 1 & 7)) * 16;
-  uint32_t xa[2] = {first + wm * MT * 2048, (first ^ 64) + wm * MT * 2048};
-  uint32_t wa[2] = {xa[0] + BM * 128 - wm * MT * 2048 + wn * NT * 2048, xa[1] + BM * 128 - wm * MT * 2048 + wn * NT * 2048};
+  // where the wave's operands lie in the first half of a step (the second: ^ 64), and the buffer that is read next
+  const int place = (lane & 15) * 128 + ((lane >> 4) ^ (lane >> 1 & 7)) * 16;
+  int next = 0;
   auto read = [&]() {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+      const char* const xs = lds + next + wm * MT * 2048 + (place ^ h * 64);
+      const char* const ws = lds + next + BM * 128 + wn * NT * 2048 + (place ^ h * 64);
 #pragma unroll
-      for (int j = 0; j < NT; ++j) a[h][j] = read_lds(wa[h] + j * 2048);
+      for (int j = 0; j < NT; ++j) a[h][j] = *reinterpret_cast<const uint4*>(ws + j * 2048);
 #pragma unroll
-      for (int i = 0; i < MT; ++i) b[h][i] = read_lds(xa[h] + i * 2048);
-      xa[h] ^= kBuf;
-      wa[h] ^= kBuf;
+      for (int i = 0; i < MT; ++i) b[h][i] = *reinterpret_cast<const uint4*>(xs + i * 2048);
     }
+    next = next + kBuf == D * kBuf ? 0 : next + kBuf;
   };
-  // LOADS: with a load of the coming step between every eight multiplications
+  // LOADS: with the loads of the coming step spread between the multiplications
   auto multiply = [&](auto loads) {
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -161,7 +155,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
         for (int j = 0; j < NT; ++j) acc[i][j] = mfma_chunks<TY>(a[h][j], b[h][i], acc[i][j]);
         if constexpr (decltype(loads)::value) {
           __builtin_amdgcn_sched_barrier(0);
-          if (i % 2 == 0) load(h * 4 + i / 2);
+#pragma unroll
+          for (int l = 0; l < kLoads; ++l)
+            if (l * 2 * MT / kLoads == h * MT + i) load(l);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -169,12 +165,10 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
   };
 
   if (steps > 0) {
-    issue();
-    if (steps > 1) {
-      issue();
-      wait_loads<kLoads>();
-    }
-    if (steps == 1) landed(0);
+#pragma unroll 1
+    for (int d = 0; d < D && d < steps; ++d) issue();
+    if (steps >= D) wait_loads<(D - 1) * kLoads>();
+    else landed(0);   // (waits for more than step 0: there are fewer than D)
     phase_ends();
     // (as few bodies as there can be without a branch between multiplications: code that runs once costs a fetch from
     // memory every few instructions, 2 us per KB)
@@ -191,9 +185,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
       phase_ends();
     } else {
       phase_ends();
-      for (; s < steps - 2; ++s) {
+      for (; s < steps - D; ++s) {
         read();
-        wait_loads<0>();   // step s + 1, not the last
+        wait_loads<(D - 2) * kLoads>();   // step s + 1, not the last
         phase_ends();
         begin_step();
         multiply(std::true_type{});
@@ -211,7 +205,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
   }
   const int row0 = m0 + wm * MT * 16;
   __syncthreads();   // (no wave reads operands any more)
-  constexpr int EM = MT / 2;
+  constexpr int EM = 4;
+  static_assert(kWaves * EM * 16 * NT * 64 <= D * kBuf, "four row tiles of every wave");
   char* mine = lds + wave * EM * 16 * NT * 64;
   if (gated) tile_epilogue<TY, MT, NT, EM, true>(p, acc, mine, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
   else tile_epilogue<TY, MT, NT, EM, false>(p, acc, mine, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
@@ -222,15 +217,21 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
 bool linear_wide_applies(const LinearParams& p, fupr_dtype dt) {
   // offsets of 32 bits from the tile's first row (gathered rows: from the first of all) and filter
   const int64_t limit = int64_t(1) << 32;
-  return dt != FUPR_F32 && (p.src ? p.x_rows : BM) * p.x_stride <= limit && BN * p.w_stride <= limit;
+  return dt != FUPR_F32 && (p.src ? p.x_rows : 256) * p.x_stride <= limit && BN * p.w_stride <= limit;
 }
 
-fupr_status launch_linear_wide(LinearParams p, fupr_dtype dt, void* stream) {
+fupr_status launch_linear_wide(LinearParams p, fupr_dtype dt, int rows, void* stream) {
   hipStream_t st = (hipStream_t)stream;
   unsigned blocks;
-  if (!count_tiles(p, BM, BN, &blocks)) return FUPR_ERR_LIMIT;
-  if (dt == FUPR_BF16) linear_wide_kernel<FUPR_BF16><<<dim3(blocks), dim3(kWaves * 64), 0, st>>>(p);
-  else linear_wide_kernel<FUPR_F16><<<dim3(blocks), dim3(kWaves * 64), 0, st>>>(p);
+  if (!count_tiles(p, rows, BN, &blocks)) return FUPR_ERR_LIMIT;
+  const dim3 grid(blocks), block(kWaves * 64);
+  if (dt == FUPR_BF16) {
+    if (rows == 256) linear_wide_kernel<FUPR_BF16, 8, 2><<<grid, block, 0, st>>>(p);
+    else linear_wide_kernel<FUPR_BF16, 4, 3><<<grid, block, 0, st>>>(p);
+  } else {
+    if (rows == 256) linear_wide_kernel<FUPR_F16, 8, 2><<<grid, block, 0, st>>>(p);
+    else linear_wide_kernel<FUPR_F16, 4, 3><<<grid, block, 0, st>>>(p);
+  }
   return launch_status("linear_wide_kernel");
 }
 
