@@ -2,13 +2,16 @@
 //
 // Why so large: a compute unit takes in 64 bytes per clock, and 128 x 128 tiles need that much to keep the matrix
 // units busy; these need half and three quarters of it.  A step of 128 bytes of every row (64 elements, whole lines)
-// goes global -> LDS as in linear_tile.hip, into D buffers.
+// goes global -> LDS as in linear_tile.hip.
 //
 // The waves' halves take turns: while the first four (one per SIMD) multiply a step from registers, the other four
 // read theirs from LDS, all of it (at 256 rows 96 registers beside 128 of accumulators).  Each phase ends in a barrier;
-// in it one half does nothing but multiply, at a raised wave priority.  Phase 2 s: the first half reads step s, the
-// second multiplies s - 1, and both ask for step s + D - 1 into the buffer that the second half has read to its end in
-// phase 2 s - 1.
+// in it one half does nothing but multiply, at a raised wave priority.  The first half reads step s in phase 2 s and
+// multiplies it in phase 2 s + 1, the second half one phase later.
+//
+// A half reads its own rows only, so they are asked for by its own waves, while it multiplies the step before whose
+// buffer (of two) it has just read; the filters (three buffers) while it reads.  That puts the same number of loads
+// into every phase, and three phases at least between asking for something and reading it.
 //
 // LDS row r (128 bytes) holds its eight chunks at chunk ^ (r / 2 & 7): operand reads cover all 64 banks once.
 #include <hip/hip_runtime.h>
@@ -43,12 +46,14 @@ __device__ __forceinline__ void load_to_lds_from(const char* base, uint32_t off,
       : "memory", "m0");
 }
 
-template <int TY, int MT, int D>
+template <int TY, int MT>
 __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParams p) {
   constexpr int kChunk = 8, kStep = 64;   // elements
-  constexpr int BM = 32 * MT, XL = BM / 64, kLoads = XL + 4, kBuf = (BM + BN) * 128;   // loads: 8 rows each, of a wave
-  __shared__ __attribute__((aligned(1024))) char lds[D * kBuf];
+  constexpr int BM = 32 * MT, kXLoads = MT / 2, kWLoads = 4, kLoads = kXLoads + kWLoads;   // of a wave, 8 rows each
+  constexpr int kXBuf = BM * 128, kWBuf = BN * 128, kW0 = 2 * kXBuf;
+  __shared__ __attribute__((aligned(1024))) char lds[2 * kXBuf + 3 * kWBuf];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wm = wave / 4, wn = wave % 4;
   const bool gated = p.w_up != nullptr;
   TilePlace at;
   if (!find_tile<BM>(p, lane, at)) return;
@@ -58,68 +63,65 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
 
   // the lane's place in every load: row lane / 8 of eight, and the chunk that is kept there
   const int chunk = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
-  uint32_t off[kLoads];
+  uint32_t xoff[kXLoads], woff[kWLoads];
   const char* xb = p.src ? p.x : p.x + (int64_t)m0 * p.x_stride;
   const char* wb = p.w + e * p.w_expert + n0 * p.w_stride;
-  const char* ub = gated ? p.w_up + e * p.w_expert + n0 * p.w_stride : wb;
 #pragma unroll
-  for (int i = 0; i < XL; ++i) {
-    const int row = min(m0 + (i * kWaves + wave) * 8 + (lane >> 3), hi - 1);
+  for (int i = 0; i < kXLoads; ++i) {
+    const int row = min(m0 + wm * MT * 16 + (i * 4 + wn) * 8 + (lane >> 3), hi - 1);
     const int from = p.src ? min(max(p.src[row], 0), p.x_rows - 1) : row - m0;
-    off[i] = (uint32_t)from * (uint32_t)p.x_stride + chunk * 16;
+    xoff[i] = (uint32_t)from * (uint32_t)p.x_stride + chunk * 16;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < kWLoads; ++i) {
     const int n = min(filter_of<NT>((i * kWaves + wave) * 8 + (lane >> 3), gated), max(n_len - n0, 1) - 1);
-    off[XL + i] = (uint32_t)n * (uint32_t)p.w_stride + chunk * 16;
+    woff[i] = (uint32_t)n * (uint32_t)p.w_stride + chunk * 16;
   }
-  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 1024;
-  // LDS rows of load i: (i * 8 + wave) * 8 ..; an odd tile of 16 is the gated layer's
-  const bool odd_tile = gated && (wave >> 1 & 1);
-  const char* fb = odd_tile ? ub : wb;
+  // LDS rows of filter load i: (i * 8 + wave) * 8 ..; an odd tile of 16 is the gated layer's
+  if (gated && (wave >> 1 & 1)) wb = p.w_up + e * p.w_expert + n0 * p.w_stride;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const uint32_t x_to = lds0 + (wm * MT * 2 + wn) * 1024, w_to = lds0 + kW0 + wave * 1024;
 
-  // One load of step `issued`.  Where the reduction ends inside a row's step, chunks behind its last one are that last
-  // one again (inside the row, and zeroed below).
-  int issued = 0;
-  uint32_t to = 0;
-  auto load = [&](int i) {
-    load_to_lds_from(i < XL ? xb : fb, off[i], lds0 + to + i * kWaves * 1024);
-  };
-  auto begin_step = [&]() {
-    if (issued == steps - 1) {
-      const int last = (k_len + kChunk - 1) / kChunk - 1;
-      const uint32_t back = max(issued * 8 + chunk - last, 0) * 16;
+  // Loads of one step after the other.  Where the reduction ends inside a row's step, chunks behind its last one are that
+  // last one again (inside the row, and zeroed below).
+  const uint32_t back = max((steps - 1) * 8 + chunk - ((k_len + kChunk - 1) / kChunk - 1), 0) * 16;
+  int xs_asked = 0, ws_asked = 0;
+  uint32_t xslot = 0, wslot = 0;
+  auto load_x = [&](int i) { load_to_lds_from(xb, xoff[i], x_to + xslot + i * 4096); };
+  auto load_w = [&](int i) { load_to_lds_from(wb, woff[i], w_to + wslot + i * kWaves * 1024); };
+  auto begin_x = [&]() {
+    if (xs_asked == steps - 1)
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) off[i] -= back;
-    }
+      for (int i = 0; i < kXLoads; ++i) xoff[i] -= back;
   };
-  auto end_step = [&]() {
-    ++issued;
+  auto end_x = [&]() {
+    ++xs_asked;
     xb += 128;
-    fb += 128;
-    to = to + kBuf == D * kBuf ? 0 : to + kBuf;
+    xslot ^= kXBuf;
   };
-  auto issue = [&]() {
-    begin_step();
+  auto ask_w = [&]() {
+    if (ws_asked == steps - 1)
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load(i);
-    end_step();
+      for (int i = 0; i < kWLoads; ++i) woff[i] -= back;
+#pragma unroll
+    for (int i = 0; i < kWLoads; ++i) load_w(i);
+    ++ws_asked;
+    wb += 128;
+    wslot = wslot + kWBuf == 3 * kWBuf ? 0 : wslot + kWBuf;
   };
-  // Step s has landed, with D - 2 later ones still in flight; zeros behind the reduction's end, in the wave's own part.
-  auto landed = [&](int s) {
-    if (s >= steps) return;
-    if (D > 2 && s + D - 2 < steps) wait_loads<(D - 2) * kLoads>();
-    else wait_loads<0>();
-    const int valid = k_len - s * kStep - chunk * kChunk;
-    if (s == steps - 1 && valid < kChunk) {
-      char* mine = lds + s % D * kBuf + wave * 1024 + lane * 16;
+  // Zeros behind the reduction's end, in what this wave has loaded of the last step (n loads, `apart` bytes from each
+  // other).
+  const int valid = k_len - (steps - 1) * kStep - chunk * kChunk;
+  auto clear = [&](uint32_t from, int n, int apart) {
+    if (valid >= kChunk) return;
 #pragma unroll 1
-      for (int i = 0; i < kLoads; ++i) {
-        uint4* v = reinterpret_cast<uint4*>(mine + i * kWaves * 1024);
-        *v = keep_first<TY>(*v, valid);
-      }
+    for (int i = 0; i < n; ++i) {
+      uint4* v = reinterpret_cast<uint4*>(lds + (from - lds0) + i * apart + lane * 16);
+      *v = keep_first<TY>(*v, valid);
     }
   };
+  auto clear_x = [&]() { clear(x_to + (steps - 1) % 2 * kXBuf, kXLoads, 4096); };
+  auto clear_w = [&]() { clear(w_to + (steps - 1) % 3 * kWBuf, kWLoads, kWaves * 1024); };
 
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   f32x4 acc[MT][NT];
@@ -127,24 +129,24 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = zero;
-  const int wm = wave / 4, wn = wave % 4;
   uint4 a[2][NT], b[2][MT];   // of the two halves of a step
-  // where the wave's operands lie in the first half of a step (the second: ^ 64), and the buffer that is read next
+  // where the wave's operands lie in the first half of a step (the second: ^ 64), and the buffers that are read next
   const int place = (lane & 15) * 128 + ((lane >> 4) ^ (lane >> 1 & 7)) * 16;
-  int next = 0;
+  int x_next = wm * MT * 2048, w_next = 0;
   auto read = [&]() {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const char* const xs = lds + next + wm * MT * 2048 + (place ^ h * 64);
-      const char* const ws = lds + next + BM * 128 + wn * NT * 2048 + (place ^ h * 64);
+      const char* const xs = lds + x_next + (place ^ h * 64);
+      const char* const ws = lds + kW0 + w_next + wn * NT * 2048 + (place ^ h * 64);
 #pragma unroll
       for (int j = 0; j < NT; ++j) a[h][j] = *reinterpret_cast<const uint4*>(ws + j * 2048);
 #pragma unroll
       for (int i = 0; i < MT; ++i) b[h][i] = *reinterpret_cast<const uint4*>(xs + i * 2048);
     }
-    next = next + kBuf == D * kBuf ? 0 : next + kBuf;
+    x_next ^= kXBuf;
+    w_next = w_next + kWBuf == 3 * kWBuf ? 0 : w_next + kWBuf;
   };
-  // LOADS: with the loads of the coming step spread between the multiplications
+  // LOADS: with the loads of x spread between the multiplications
   auto multiply = [&](auto loads) {
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -155,9 +157,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
         for (int j = 0; j < NT; ++j) acc[i][j] = mfma_chunks<TY>(a[h][j], b[h][i], acc[i][j]);
         if constexpr (decltype(loads)::value) {
           __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int l = 0; l < kLoads; ++l)
-            if (l * 2 * MT / kLoads == h * MT + i) load(l);
+          if ((h * MT + i) % 4 == 1) load_x((h * MT + i) / 4);
           __builtin_amdgcn_sched_barrier(0);
         }
       }
@@ -165,48 +165,58 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
   };
 
   if (steps > 0) {
+    const bool late = wm != 0;
 #pragma unroll 1
-    for (int d = 0; d < D && d < steps; ++d) issue();
-    if (steps >= D) wait_loads<(D - 1) * kLoads>();
-    else landed(0);   // (waits for more than step 0: there are fewer than D)
+    for (int d = 0; d < 2 && d < steps; ++d) {
+      ask_w();
+      begin_x();
+#pragma unroll
+      for (int i = 0; i < kXLoads; ++i) load_x(i);
+      end_x();
+    }
+    if (steps > 1) {
+      wait_loads<kLoads>();
+    } else {
+      wait_loads<0>();
+      clear_w();
+      clear_x();
+    }
     phase_ends();
+    if (late) phase_ends();
     // (as few bodies as there can be without a branch between multiplications: code that runs once costs a fetch from
     // memory every few instructions, 2 us per KB)
     int s = 0;
-    if (wave < kWaves / 2) {
-      while (s < steps) {
-        read();
-        if (s >= 1 && issued < steps) issue();
-        phase_ends();
-        multiply(std::false_type{});
-        landed(++s);
-        phase_ends();
-      }
+    for (; s < steps - 2; ++s) {
+      read();
+      ask_w();                  // of step s + 2
+      wait_loads<kLoads>();     // filters of step s + 1 have landed
       phase_ends();
-    } else {
+      begin_x();                // of step s + 2
+      multiply(std::true_type{});
+      end_x();
+      wait_loads<kLoads>();     // rows of step s + 1
       phase_ends();
-      for (; s < steps - D; ++s) {
-        read();
-        wait_loads<(D - 2) * kLoads>();   // step s + 1, not the last
-        phase_ends();
-        begin_step();
-        multiply(std::true_type{});
-        end_step();
-        phase_ends();
-      }
-      while (s < steps) {
-        read();
-        landed(++s);
-        phase_ends();
-        multiply(std::false_type{});
-        phase_ends();
-      }
     }
+    for (; s < steps; ++s) {
+      read();
+      if (s + 1 < steps) {
+        wait_loads<kXLoads>();
+        clear_w();
+      }
+      phase_ends();
+      multiply(std::false_type{});
+      if (s + 1 < steps) {
+        wait_loads<0>();
+        clear_x();
+      }
+      phase_ends();
+    }
+    if (!late) phase_ends();
   }
   const int row0 = m0 + wm * MT * 16;
   __syncthreads();   // (no wave reads operands any more)
   constexpr int EM = 4;
-  static_assert(kWaves * EM * 16 * NT * 64 <= D * kBuf, "four row tiles of every wave");
+  static_assert(kWaves * EM * 16 * NT * 64 <= sizeof(lds), "four row tiles of every wave");
   char* mine = lds + wave * EM * 16 * NT * 64;
   if (gated) tile_epilogue<TY, MT, NT, EM, true>(p, acc, mine, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
   else tile_epilogue<TY, MT, NT, EM, false>(p, acc, mine, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
@@ -226,11 +236,11 @@ fupr_status launch_linear_wide(LinearParams p, fupr_dtype dt, int rows, void* st
   if (!count_tiles(p, rows, BN, &blocks)) return FUPR_ERR_LIMIT;
   const dim3 grid(blocks), block(kWaves * 64);
   if (dt == FUPR_BF16) {
-    if (rows == 256) linear_wide_kernel<FUPR_BF16, 8, 2><<<grid, block, 0, st>>>(p);
-    else linear_wide_kernel<FUPR_BF16, 4, 3><<<grid, block, 0, st>>>(p);
+    if (rows == 256) linear_wide_kernel<FUPR_BF16, 8><<<grid, block, 0, st>>>(p);
+    else linear_wide_kernel<FUPR_BF16, 4><<<grid, block, 0, st>>>(p);
   } else {
-    if (rows == 256) linear_wide_kernel<FUPR_F16, 8, 2><<<grid, block, 0, st>>>(p);
-    else linear_wide_kernel<FUPR_F16, 4, 3><<<grid, block, 0, st>>>(p);
+    if (rows == 256) linear_wide_kernel<FUPR_F16, 8><<<grid, block, 0, st>>>(p);
+    else linear_wide_kernel<FUPR_F16, 4><<<grid, block, 0, st>>>(p);
   }
   return launch_status("linear_wide_kernel");
 }
