@@ -108,18 +108,16 @@ __device__ __forceinline__ void store_row(const LinearParams& p, int64_t row, in
   }
 }
 
-// From a wave's accumulators to y.  They pass through the wave's own part of LDS, EM row tiles at a time, so that eight
-// consecutive columns of a row meet in a lane and the rest is a loop that is not written out for every register: a
-// version straight from the registers spilled them and took 10 us more for a tile of 256 x 256.  LDS rows of NT * 4
-// chunks of four columns (gated: the gate's half, then the other's) hold chunk c at c ^ (row modulo their number).
-// nb: the wave's first column.
-template <int TY, int MT, int NT, int EM, bool GATED>
-__device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4 (&acc)[MT][NT], char* lds, int e, int hi,
-                                              int row0, int nb, int n_len, int lane) {
+// What stands between a wave's sums and y: bias, activation, gate, residual, rounding.  The sums come from the wave's
+// own part of LDS, where eight consecutive columns of a row meet in a lane and the work is a loop that is not written
+// out for every register: a version straight from the registers spilled them and took 10 us more for a tile of
+// 256 x 256.  `rows` rows of CHUNKS chunks of four columns (gated: the gate's half, then the other's), chunk c at
+// c ^ (row modulo CHUNKS).  first: the row of y, nb: the column where they begin.
+template <int TY, int CHUNKS, bool GATED>
+__device__ __forceinline__ void finish_rows(const LinearParams& p, const char* lds, int rows, int e, int hi, int first, int nb,
+                                            int n_len, int lane) {
   constexpr bool FINE = TY == FUPR_F32;
-  constexpr int kChunks = NT * 4, kCols = GATED ? NT * 8 : NT * 16;   // of a row
-  constexpr int kLanes = kCols / 8, kRows = 64 / kLanes, kTurns = EM * 16 / kRows;
-  static_assert(MT % EM == 0, "whole parts");
+  constexpr int kCols = GATED ? CHUNKS * 2 : CHUNKS * 4, kLanes = kCols / 8;   // of a row
   const int c = lane % kLanes, n = nb + c * 8;
   float bias[8], up[8];
 #pragma unroll
@@ -127,9 +125,44 @@ __device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4
     bias[i] = p.bias && n + i < n_len ? p.bias[(int64_t)e * p.N + n + i] : 0.f;
     up[i] = GATED && p.bias_up && n + i < n_len ? p.bias_up[(int64_t)e * p.N + n + i] : 0.f;
   }
+#pragma unroll 1
+  for (int r = lane / kLanes; r < rows; r += 64 / kLanes) {
+    const int row = first + r;
+    const Addend<TY> add = load_addend<TY>(p, row, n, row < hi);
+    const char* from = lds + r * CHUNKS * 16;
+    float v[8], u[8];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const f32x4 a = *reinterpret_cast<const f32x4*>(from + (((c * 2 + q) ^ r) & (CHUNKS - 1)) * 16);
+      f32x4 b = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (GATED) b = *reinterpret_cast<const f32x4*>(from + (((CHUNKS / 2 + c * 2 + q) ^ r) & (CHUNKS - 1)) * 16);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[q * 4 + i] = a[i] + bias[q * 4 + i];
+        u[q * 4 + i] = b[i] + up[q * 4 + i];
+      }
+    }
+    with_activation(p.act, [&](auto act) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = activate<FINE, decltype(act)::value>(v[i]);
+    });
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (GATED) v[i] *= u[i];
+      if (n + i >= n_len) v[i] = 0.f;   // columns that pruning took from this expert
+    }
+    if (row < hi && n < p.N) store_row<TY>(p, row, n, v, add);
+  }
+}
+
+// From a wave's accumulators of 16 x 16 tiles to y, EM row tiles at a time.
+template <int TY, int MT, int NT, int EM, bool GATED>
+__device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4 (&acc)[MT][NT], char* lds, int e, int hi,
+                                              int row0, int nb, int n_len, int lane) {
+  constexpr int kChunks = NT * 4;
+  static_assert(MT % EM == 0, "whole parts");
 #pragma unroll
   for (int part = 0; part < MT / EM; ++part) {
-    const int first = row0 + part * EM * 16 + lane / kLanes;
 #pragma unroll
     for (int i = 0; i < EM; ++i)
 #pragma unroll
@@ -138,34 +171,7 @@ __device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4
         const int at = GATED ? (t & 1) * (kChunks / 2) + g * (NT / 2) + t / 2 : g * NT + t;
         *reinterpret_cast<f32x4*>(lds + (i * 16 + r) * kChunks * 16 + ((at ^ r) & (kChunks - 1)) * 16) = acc[part * EM + i][t];
       }
-#pragma unroll 1
-    for (int turn = 0; turn < kTurns; ++turn) {
-      const int r = turn * kRows + lane / kLanes, row = first + turn * kRows;
-      const char* from = lds + r * kChunks * 16;
-      float v[8], u[8];
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(from + (((c * 2 + q) ^ r) & (kChunks - 1)) * 16);
-        f32x4 b = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (GATED) b = *reinterpret_cast<const f32x4*>(from + (((kChunks / 2 + c * 2 + q) ^ r) & (kChunks - 1)) * 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[q * 4 + i] = a[i] + bias[q * 4 + i];
-          u[q * 4 + i] = b[i] + up[q * 4 + i];
-        }
-      }
-      const Addend<TY> add = load_addend<TY>(p, row, n, row < hi);
-      with_activation(p.act, [&](auto act) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = activate<FINE, decltype(act)::value>(v[i]);
-      });
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (GATED) v[i] *= u[i];
-        if (n + i >= n_len) v[i] = 0.f;   // columns that pruning took from this expert
-      }
-      if (row < hi && n < p.N) store_row<TY>(p, row, n, v, add);
-    }
+    finish_rows<TY, kChunks, GATED>(p, lds, EM * 16, e, hi, row0 + part * EM * 16, nb, n_len, lane);
   }
 }
 
