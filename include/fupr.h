@@ -762,8 +762,9 @@ void fupr_graph_destroy(fupr_graph* g);
  *   resident_rows = 0                             models made meanwhile: the one-kernel schedule without its
  *                                                 kernel for networks of 3 x 3 convolutions
  *   res_item = "M/FT/nsteps:MTxNT,..."            work-item shapes of the one-kernel schedule
- *   linear_rows = <rows>                          most rows of a linear layer (of the average expert) for the kernel
- *                                                 of few rows
+ *   linear_tile = 0 .. 7                          tile of the linear layers, rows x filters: 16 x 16 (weights straight
+ *                                                 into registers), 32 x 32, 32 x 64, 64 x 64, 64 x 128, 128 x 128,
+ *                                                 128 x 256, 256 x 256; ignored where a tile cannot serve the call
  *   debug = 1                                     planner decisions and HIP error text on stderr
  * Errors: NULL, ARG (unknown name, value of 128 characters or more).
  */

@@ -1,5 +1,6 @@
 // Entry points of the linear layers: argument checks on the host, then one launch.
 #include "linear.h"
+#include "tuning.h"
 
 #include <cstdint>
 
@@ -77,6 +78,62 @@ bool overlaps_weights(const fupr_matrix& y, const fupr_linear& op, const void* w
          py < pw + (uintptr_t)(n * bytes_of(op.dt));
 }
 
+// What a tile costs, in microseconds: `begin` from its first instruction to its first multiplication and from the last one
+// to its results, and `lo` or `hi` for 64 bytes of every row, `lo` where the workgroups leave room on the card, `hi`
+// where they fill it (each measured: layers of 256 to 4096 filters of 300 to 4096 weights on 16 to 8192 rows).
+struct TileCost {
+  int rows, cols, at_once;    // at_once: workgroups of a compute unit
+  float begin, lo, hi;        // 16-bit types
+  float lo32, hi32;           // single precision; 0: not for it
+};
+constexpr TileCost kCosts[kLinearTiles] = {
+    {16, 16, 1, 0.7f, 0.055f, 0.055f, 0.055f, 0.055f},
+    {32, 32, 1, 2.0f, 0.045f, 0.060f, 0.085f, 0.095f},
+    {32, 64, 2, 2.2f, 0.070f, 0.132f, 0.14f, 0.26f},
+    {64, 64, 2, 2.8f, 0.118f, 0.25f, 0.27f, 0.52f},
+    {64, 128, 2, 4.0f, 0.19f, 0.48f, 0.48f, 0.92f},
+    {128, 128, 2, 4.8f, 0.32f, 0.62f, 0.93f, 1.9f},
+    {128, 256, 1, 6.0f, 0.29f, 0.42f, 0.f, 0.f},
+    {256, 256, 1, 8.7f, 0.54f, 0.72f, 0.f, 0.f},
+};
+
+// The kernel whose tiles are through first: small ones put more compute units to work, large ones read less for
+// every multiplication.
+LinearTile choose_tile(const LinearParams& p, fupr_dtype dt) {
+  const bool may[2] = {linear_rows_applies(p), linear_wide_applies(p, dt)};
+  auto applies = [&](int t) { return t == kRows16x16 ? may[0] : t >= kWide128x256 ? may[1] : true; };
+  if (tuning_any()) {
+    const int forced = tuning_int("linear_tile", -1);
+    if (forced >= 0 && forced < kLinearTiles && applies(forced)) return (LinearTile)forced;
+  }
+  const float units = (float)((p.K * (dt == FUPR_F32 ? 4 : 2) + 63) / 64);
+  float best = 0.f;
+  int which = -1;
+  for (int t = 0; t < kLinearTiles; ++t) {
+    const TileCost& c = kCosts[t];
+    if (!applies(t)) continue;
+    // (the rows kernel has 16 filters of both layers of a gated one, the others half as many of each)
+    const int cols = p.w_up && t != kRows16x16 ? c.cols / 2 : c.cols;
+    float rows = (float)((p.M - 1) / c.rows + 1);
+    if (p.offsets) {
+      // the counts are on the device: as if every expert that can have rows left half a tile empty
+      const float begun = (float)(p.E < p.M ? p.E : p.M), about = (float)p.M / c.rows + 0.5f * begun;
+      rows = about > begun ? about : begun;
+    }
+    const float lo = (dt == FUPR_F32 ? c.lo32 : c.lo) * (p.w_up && t == kRows16x16 ? 1.6f : 1.f);
+    const float hi = (dt == FUPR_F32 ? c.hi32 : c.hi) * (p.w_up && t == kRows16x16 ? 1.6f : 1.f);
+    const float fill = rows * (float)((p.N - 1) / cols + 1) / (float)(256 * c.at_once);
+    const float full = (float)(int)fill, rest = fill - full, more = rest > 0.5f ? 2.f * rest - 1.f : 0.f;
+    const float cost = full * (c.begin + units * hi) + (rest > 0.f ? c.begin + units * (lo + (hi - lo) * more) : 0.f) +
+                       (t == kRows16x16 ? 0.5f : 0.f);
+    if (which < 0 || cost < best) {
+      best = cost;
+      which = t;
+    }
+  }
+  return (LinearTile)which;
+}
+
 fupr_status run_linear(const fupr_linear& op, int32_t E, int64_t expert_stride, const int32_t* n_len,
                        const int32_t* k_len, const fupr_matrix& x, const int32_t* offsets, const int32_t* src,
                        const fupr_matrix* res, const fupr_matrix& y, void* workspace, size_t workspace_bytes,
@@ -124,7 +181,13 @@ fupr_status run_linear(const fupr_linear& op, int32_t E, int64_t expert_stride, 
   p.x_rows = x.rows;
   p.act = op.act;
   p.y_f32 = y.dt == FUPR_F32;
-  return linear_rows_applies(p, op.dt) ? launch_linear_rows(p, op.dt, stream) : launch_linear_tile(p, op.dt, stream);
+  const LinearTile tile = choose_tile(p, op.dt);
+  switch (tile) {
+    case kRows16x16: return launch_linear_rows(p, op.dt, stream);
+    case kWide128x256: return launch_linear_wide(p, op.dt, 128, stream);
+    case kWide256x256: return launch_linear_wide(p, op.dt, 256, stream);
+    default: return launch_linear_tile(p, op.dt, tile, stream);
+  }
 }
 
 }  // namespace

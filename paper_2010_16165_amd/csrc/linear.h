@@ -27,15 +27,26 @@ struct LinearParams {
   int m_tiles, n_tiles;    // of the launch: an upper bound on the row tiles of all experts
 };
 
-// linear_tile.hip: tiles of rows and filters staged through LDS.
-fupr_status launch_linear_tile(LinearParams p, fupr_dtype dt, void* stream);
+// The most row tiles of BM rows that a launch can have: of experts one begun by every one that can have a row, the
+// others full.
+inline int linear_row_tiles(const LinearParams& p, int BM) {
+  if (!p.offsets) return (p.M - 1) / BM + 1;
+  const int begun = p.E < p.M ? p.E : p.M;
+  return begun + (p.M - begun) / BM;
+}
+
+// The kernels' tiles, rows x filters.
+enum LinearTile { kRows16x16, kTile32x32, kTile32x64, kTile64x64, kTile64x128, kTile128x128, kWide128x256, kWide256x256, kLinearTiles };
+
+// linear_tile.hip: tiles of rows and filters staged through LDS, those of LinearTile named kTile*.
+fupr_status launch_linear_tile(LinearParams p, fupr_dtype dt, LinearTile tile, void* stream);
 
 // linear_wide.hip: tiles of 256 or 128 rows x 256 filters, 16-bit types.  linear_wide_applies: of these types and strides.
 bool linear_wide_applies(const LinearParams& p, fupr_dtype dt);
 fupr_status launch_linear_wide(LinearParams p, fupr_dtype dt, int rows, void* stream);
 
-// linear_rows.hip: few rows, bound by reading the weights once.  linear_rows_applies: of these sizes and strides.
-bool linear_rows_applies(const LinearParams& p, fupr_dtype dt);
+// linear_rows.hip: weights straight into the operand registers.  linear_rows_applies: of these sizes and strides.
+bool linear_rows_applies(const LinearParams& p);
 fupr_status launch_linear_rows(LinearParams p, fupr_dtype dt, void* stream);
 
 // linear.cpp: argument checks that the entry points share.

@@ -113,8 +113,8 @@ __device__ __forceinline__ void store_row(const LinearParams& p, int64_t row, in
 // out for every register: a version straight from the registers spilled them and took 10 us more for a tile of
 // 256 x 256.  `rows` rows of CHUNKS chunks of four columns (gated: the gate's half, then the other's), chunk c at
 // c ^ (row modulo CHUNKS).  first: the row of y, nb: the column where they begin.
-template <int TY, int CHUNKS, bool GATED>
-__device__ __forceinline__ void finish_rows(const LinearParams& p, const char* lds, int rows, int e, int hi, int first, int nb,
+template <int TY, int CHUNKS, int KS, bool GATED>
+__device__ __forceinline__ void finish_rows(const LinearParams& p, const char* lds, int apart, int from_row, int rows, int e, int hi, int first, int nb,
                                             int n_len, int lane) {
   constexpr bool FINE = TY == FUPR_F32;
   constexpr int kCols = GATED ? CHUNKS * 2 : CHUNKS * 4, kLanes = kCols / 8;   // of a row
@@ -126,16 +126,21 @@ __device__ __forceinline__ void finish_rows(const LinearParams& p, const char* l
     up[i] = GATED && p.bias_up && n + i < n_len ? p.bias_up[(int64_t)e * p.N + n + i] : 0.f;
   }
 #pragma unroll 1
-  for (int r = lane / kLanes; r < rows; r += 64 / kLanes) {
+  for (int r = from_row + lane / kLanes; r < rows; r += 64 / kLanes) {
     const int row = first + r;
     const Addend<TY> add = load_addend<TY>(p, row, n, row < hi);
     const char* from = lds + r * CHUNKS * 16;
     float v[8], u[8];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(from + (((c * 2 + q) ^ r) & (CHUNKS - 1)) * 16);
-      f32x4 b = {0.f, 0.f, 0.f, 0.f};
-      if constexpr (GATED) b = *reinterpret_cast<const f32x4*>(from + (((CHUNKS / 2 + c * 2 + q) ^ r) & (CHUNKS - 1)) * 16);
+      const int at_a = (((c * 2 + q) ^ r) & (CHUNKS - 1)) * 16, at_b = (((CHUNKS / 2 + c * 2 + q) ^ r) & (CHUNKS - 1)) * 16;
+      f32x4 a = *reinterpret_cast<const f32x4*>(from + at_a), b = {0.f, 0.f, 0.f, 0.f};
+      if constexpr (GATED) b = *reinterpret_cast<const f32x4*>(from + at_b);
+#pragma unroll
+      for (int k = 1; k < KS; ++k) {
+        a += *reinterpret_cast<const f32x4*>(from + k * apart + at_a);
+        if constexpr (GATED) b += *reinterpret_cast<const f32x4*>(from + k * apart + at_b);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         v[q * 4 + i] = a[i] + bias[q * 4 + i];
@@ -156,11 +161,12 @@ __device__ __forceinline__ void finish_rows(const LinearParams& p, const char* l
 }
 
 // From a wave's accumulators of 16 x 16 tiles to y, EM row tiles at a time.
-template <int TY, int MT, int NT, int EM, bool GATED>
-__device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4 (&acc)[MT][NT], char* lds, int e, int hi,
-                                              int row0, int nb, int n_len, int lane) {
+template <int TY, int MT, int NT, int EM, int KS, bool GATED>
+__device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4 (&acc)[MT][NT], char* lds, int apart,
+                                              int group, int e, int hi, int row0, int nb, int n_len, int lane) {
   constexpr int kChunks = NT * 4;
-  static_assert(MT % EM == 0, "whole parts");
+  static_assert(MT % EM == 0 && (KS == 1 || EM == MT) && EM * 16 % KS == 0, "whole parts");
+  char* const own = lds + group * apart;
 #pragma unroll
   for (int part = 0; part < MT / EM; ++part) {
 #pragma unroll
@@ -169,9 +175,10 @@ __device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4
       for (int t = 0; t < NT; ++t) {
         const int r = lane & 15, g = lane >> 4;
         const int at = GATED ? (t & 1) * (kChunks / 2) + g * (NT / 2) + t / 2 : g * NT + t;
-        *reinterpret_cast<f32x4*>(lds + (i * 16 + r) * kChunks * 16 + ((at ^ r) & (kChunks - 1)) * 16) = acc[part * EM + i][t];
+        *reinterpret_cast<f32x4*>(own + (i * 16 + r) * kChunks * 16 + ((at ^ r) & (kChunks - 1)) * 16) = acc[part * EM + i][t];
       }
-    finish_rows<TY, kChunks, GATED>(p, lds, EM * 16, e, hi, row0 + part * EM * 16, nb, n_len, lane);
+    if constexpr (KS > 1) __syncthreads();
+    finish_rows<TY, kChunks, KS, GATED>(p, lds, apart, group * (EM * 16 / KS), (group + 1) * (EM * 16 / KS), e, hi, row0 + part * EM * 16, nb, n_len, lane);
   }
 }
 
@@ -179,13 +186,7 @@ __device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4
 inline bool count_tiles(LinearParams& p, int BM, int BN, unsigned* blocks) {
   const int cols = p.w_up ? BN / 2 : BN;
   p.n_tiles = (p.N + cols - 1) / cols;
-  if (p.offsets) {
-    // at most: one tile begun by every expert that can have a row, the others full
-    const int begun = p.E < p.M ? p.E : p.M;
-    p.m_tiles = begun + (p.M - begun) / BM;
-  } else {
-    p.m_tiles = (p.M + BM - 1) / BM;
-  }
+  p.m_tiles = linear_row_tiles(p, BM);
   const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
   if (tiles > 0x7fffff00) return false;
   *blocks = (unsigned)((tiles + 7) / 8 * 8);

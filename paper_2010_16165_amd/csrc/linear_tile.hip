@@ -19,7 +19,6 @@
 #include <type_traits>
 
 #include "linear_tile.h"
-#include "tuning.h"
 
 namespace fupr {
 
@@ -27,10 +26,10 @@ fupr_status launch_status(const char* what);
 
 namespace {
 
-template <int TY_, int WM_, int WN_, int MT_, int NT_, int U_, int D_>
+template <int TY_, int WM_, int WN_, int MT_, int NT_, int U_, int D_, int KS_>
 struct TileGeom {
-  static constexpr int TY = TY_, WM = WM_, WN = WN_, MT = MT_, NT = NT_, U = U_, D = D_;
-  static constexpr int waves = WM * WN, threads = waves * 64;
+  static constexpr int TY = TY_, WM = WM_, WN = WN_, MT = MT_, NT = NT_, U = U_, D = D_, KS = KS_;
+  static constexpr int waves = WM * WN, threads = KS * waves * 64;   // waves: of a group
   static constexpr int BM = WM * MT * 16, BN = WN * NT * 16;
   static constexpr int xl = BM / 16 / waves, wl = BN / 16 / waves;   // loads of a wave and unit (16 rows each)
   static_assert(xl * 16 * waves == BM && wl * 16 * waves == BN && NT % 2 == 0, "whole loads, pairs of tiles");
@@ -42,9 +41,11 @@ struct TileGeom {
 
 template <class G>
 __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams p) {
-  constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, U = G::U, D = G::D;
-  __shared__ __attribute__((aligned(1024))) char lds[D * G::buf];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int BM = G::BM, BN = G::BN, MT = G::MT, NT = G::NT, U = G::U, D = G::D, KS = G::KS;
+  __shared__ __attribute__((aligned(1024))) char lds_all[KS * D * G::buf];
+  const int lane = threadIdx.x & 63, of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group = of_all / G::waves, wave = of_all % G::waves;
+  char* const lds = lds_all + group * D * G::buf;
   const bool gated = p.w_up != nullptr;
   const int cols = gated ? BN / 2 : BN;   // of y, in a tile
 
@@ -52,7 +53,7 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
   if (!find_tile<BM>(p, lane, at)) return;
   const int e = at.e, hi = at.hi, m0 = at.m0, n_len = at.n_len, k_len = at.k_len;
   const int n0 = at.nt * cols;
-  const int units = n0 < n_len ? (k_len + G::per_unit - 1) / G::per_unit : 0;
+  const int units = n0 < n_len ? (k_len + KS * G::per_unit - 1) / (KS * G::per_unit) : 0;   // of a group
 
   // the lane's place in every load: row lane / 4 of sixteen, and the chunk that is kept there
   const int chunk = (lane & 3) ^ (lane >> 3 & 3);
@@ -61,13 +62,13 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
   for (int i = 0; i < G::xl; ++i) {
     int row = min(m0 + (i * G::waves + wave) * 16 + (lane >> 2), hi - 1);
     if (p.src) row = min(max(p.src[row], 0), p.x_rows - 1);
-    from[i] = p.x + row * p.x_stride + chunk * 16;
+    from[i] = p.x + row * p.x_stride + group * 64 + chunk * 16;
   }
 #pragma unroll
   for (int i = 0; i < G::wl; ++i) {
     const int r = (i * G::waves + wave) * 16 + (lane >> 2);
     const char* w = gated && (r >> 4 & 1) ? p.w_up : p.w;
-    from[G::xl + i] = w + e * p.w_expert + min(n0 + filter_of<NT>(r, gated), max(n_len, 1) - 1) * p.w_stride + chunk * 16;
+    from[G::xl + i] = w + e * p.w_expert + min(n0 + filter_of<NT>(r, gated), max(n_len, 1) - 1) * p.w_stride + group * 64 + chunk * 16;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 1024;
 
@@ -76,12 +77,12 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
   int issued = 0, to = 0;
   auto load = [&](int i) {
     load_to_lds(from[i], lds0 + to + i * G::waves * 1024);
-    from[i] += 64;
+    from[i] += KS * 64;
   };
   auto begin_unit = [&]() {
     if (issued == units - 1) {
       const int last = (k_len + G::per_chunk - 1) / G::per_chunk - 1;
-      const int back = max(issued * 4 + chunk - last, 0) * 16;
+      const int back = max((issued * KS + group) * 4 + chunk - last, 0) * 16;
 #pragma unroll
       for (int i = 0; i < G::loads; ++i) from[i] -= back;
     }
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
   };
   // Zeros behind the reduction's end, in the wave's own part of the last unit's buffer, which has landed.
   auto clear_tail = [&](int buf) {
-    const int valid = k_len - (units - 1) * G::per_unit - chunk * G::per_chunk;
+    const int valid = k_len - ((units - 1) * KS + group) * G::per_unit - chunk * G::per_chunk;
     if (valid >= G::per_chunk) return;
     char* mine = lds + buf + wave * 1024 + lane * 16;
 #pragma unroll 1
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
       *v = keep_first<G::TY>(*v, valid);
     }
   };
-  const bool ragged = k_len % G::per_unit != 0;
+  const bool ragged = k_len % (KS * G::per_unit) != 0;
 
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   f32x4 acc[MT][NT];
@@ -202,9 +203,10 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
   __syncthreads();   // (no wave reads operands any more)
   constexpr int kMine = 16 * NT * 64;   // bytes of a row tile of accumulators
   constexpr int EM = G::waves * MT * kMine <= D * G::buf ? MT : G::waves * MT * kMine <= 2 * D * G::buf ? MT / 2 : MT / 4;
-  char* mine = lds + wave * EM * kMine;
-  if (gated) tile_epilogue<G::TY, MT, NT, EM, true>(p, acc, mine, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
-  else tile_epilogue<G::TY, MT, NT, EM, false>(p, acc, mine, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
+  constexpr int apart = D * G::buf;
+  char* mine = lds_all + wave * EM * kMine;
+  if (gated) tile_epilogue<G::TY, MT, NT, EM, KS, true>(p, acc, mine, apart, group, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
+  else tile_epilogue<G::TY, MT, NT, EM, KS, false>(p, acc, mine, apart, group, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
 }
 
 template <class G>
@@ -216,25 +218,24 @@ fupr_status launch_as(LinearParams p, hipStream_t st) {
 }
 
 template <int TY>
-fupr_status launch_type(const LinearParams& p, hipStream_t st) {
-  switch (tuning_any() ? tuning_int("linear_tile", 0) : 0) {
-#ifdef TILES
-    TILES
-#endif
-    default: return launch_as<TileGeom<TY, 2, 2, 4, 4, 2, 4>>(p, st);
+fupr_status launch_type(const LinearParams& p, LinearTile tile, hipStream_t st) {
+  switch (tile) {
+    case kTile32x32: return launch_as<TileGeom<TY, 1, 1, 2, 2, 2, 6, 4>>(p, st);
+    case kTile32x64: return launch_as<TileGeom<TY, 1, 2, 2, 2, 2, 6, 2>>(p, st);
+    case kTile64x64: return launch_as<TileGeom<TY, 2, 2, 2, 2, 2, 8, 1>>(p, st);
+    case kTile64x128: return launch_as<TileGeom<TY, 2, 2, 2, 4, 2, 6, 1>>(p, st);
+    default: return launch_as<TileGeom<TY, 2, 2, 4, 4, 2, 4, 1>>(p, st);
   }
 }
 
 }  // namespace
 
-fupr_status launch_linear_tile(LinearParams p, fupr_dtype dt, void* stream) {
-  const int forced = tuning_any() ? tuning_int("linear_tile", 0) : 0;
-  if ((forced == 99 || forced == 98) && linear_wide_applies(p, dt)) return launch_linear_wide(p, dt, forced == 99 ? 256 : 128, stream);
+fupr_status launch_linear_tile(LinearParams p, fupr_dtype dt, LinearTile tile, void* stream) {
   hipStream_t st = (hipStream_t)stream;
   switch (dt) {
-    case FUPR_BF16: return launch_type<FUPR_BF16>(p, st);
-    case FUPR_F16: return launch_type<FUPR_F16>(p, st);
-    default: return launch_type<FUPR_F32>(p, st);
+    case FUPR_BF16: return launch_type<FUPR_BF16>(p, tile, st);
+    case FUPR_F16: return launch_type<FUPR_F16>(p, tile, st);
+    default: return launch_type<FUPR_F32>(p, tile, st);
   }
 }
 

@@ -218,8 +218,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
   constexpr int EM = 4;
   static_assert(kWaves * EM * 16 * NT * 64 <= sizeof(lds), "four row tiles of every wave");
   char* mine = lds + wave * EM * 16 * NT * 64;
-  if (gated) tile_epilogue<TY, MT, NT, EM, true>(p, acc, mine, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
-  else tile_epilogue<TY, MT, NT, EM, false>(p, acc, mine, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
+  if (gated) tile_epilogue<TY, MT, NT, EM, 1, true>(p, acc, mine, 0, 0, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
+  else tile_epilogue<TY, MT, NT, EM, 1, false>(p, acc, mine, 0, 0, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
 }
 
 }  // namespace

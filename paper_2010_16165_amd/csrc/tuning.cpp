@@ -46,8 +46,7 @@ Switch g_switches[] = {
     {"split", false, {0}},           // sub-batches of the per-operator schedule
     {"resident_rows", false, {0}},   // 0: the one-kernel schedule without its kernel of row layers
     {"res_item", false, {0}},        // work-item shapes of the one-kernel schedule
-    {"linear_tile", false, {0}},     // index of the tile of linear layers on many rows
-    {"linear_rows", false, {0}},     // most rows of a linear layer (or average expert) for the few-rows kernel
+    {"linear_tile", false, {0}},     // index of the tile of linear layers (linear.h)
     {"debug", false, {0}},           // non-empty: planner and HIP error text on stderr
 };
 

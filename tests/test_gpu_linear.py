@@ -253,6 +253,69 @@ def test_expert_linear_stays_inside_its_tensors(fx, rows, n):
             check(wide(y[:8]), want, bound)
 
 
+@pytest.fixture(params=range(8), ids=["16x16", "32x32", "32x64", "64x64", "64x128", "128x128", "128x256", "256x256"])
+def tile(fx, request):
+    """Every call with this tile, whatever the rule would take."""
+    B, _ = fx
+    B.fupr_tuning_set("linear_tile", str(request.param))
+    yield request.param
+    B.fupr_tuning_set("linear_tile", None)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_every_tile(fx, tile, dtype):
+    """Reductions that end in the first step, in the second, in the first of a group of waves, and far behind; tiles
+    with one row or filter and with all."""
+    B, torch = fx
+    dt = type_of(torch, dtype)
+    eps, own = torch.finfo(dt).eps, 2.0 ** -20 if dtype == "f32" else 2.0 ** -18
+    for M, N, K in ((1, 1, 1), (33, 70, 24), (130, 300, 136), (256, 256, 128), (300, 270, 203), (515, 520, 72), (65, 129, 1101),
+                    (257, 40, 700)):
+        rng = np.random.default_rng([M, N, K])
+        x = rows_of(torch, rng.standard_normal((M, K)), dt, 8)
+        w, wu = (rows_of(torch, rng.standard_normal((N, K)) / math.sqrt(K), dt) for _ in range(2))
+        b, bu = (torch.from_numpy(rng.standard_normal(N).astype(np.float32)).cuda() for _ in range(2))
+        res = rows_of(torch, rng.standard_normal((M, N)), dt)
+        for gated in (False, True):
+            op = B.Linear(w, b, wu if gated else None, bu if gated else None, B.ACTIVATIONS["silu" if gated else "none"])
+            y = rows_of(torch, np.full((M, N), 7.0), dt, 8)
+            B.fupr_linear_fused(op, x, y, res, op.workspace(M))
+            want, bound = reference(wide(x), wide(w), wide(b), wide(wu) if gated else None, wide(bu) if gated else None,
+                                    "silu" if gated else "none", wide(res), eps, own)
+            check(wide(y), want, bound)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("load", ["idle", "tall"])
+def test_every_tile_of_experts(fx, tile, load, dtype):
+    """Ragged rows and widths through src; the lengths of the reduction lie in different steps."""
+    B, torch = fx
+    dt = type_of(torch, dtype)
+    counts = COUNTS[load]
+    E, total, N, K, T = len(counts), sum(counts), 270, 210, 60
+    rng = np.random.default_rng(E)
+    off = np.concatenate([[0], np.cumsum(counts)])
+    w, wu = (rows_of(torch, rng.standard_normal((E, N, K)) / 14, dt) for _ in range(2))
+    x = rows_of(torch, rng.standard_normal((T, K)), dt)
+    n_len, k_len = rng.integers(0, N + 1, E), rng.integers(0, K + 1, E)
+    n_len[0], k_len[0] = N, K
+    src = rng.integers(0, T, total).astype(np.int32)
+    for gated in (False, True):
+        op = B.ExpertLinear(w, None, wu if gated else None, None, B.ACTIVATIONS["silu" if gated else "none"],
+                            *(torch.from_numpy(v.astype(np.int32)).cuda() for v in (n_len, k_len)))
+        y = rows_of(torch, np.full((total, N), 7.0), dt)
+        B.fupr_expert_linear_fused(op, x, torch.from_numpy(off.astype(np.int32)).cuda(), torch.from_numpy(src).cuda(), y,
+                                   op.workspace(total))
+        got, xs, ws, wus = (wide(t) for t in (y, x, w, wu))
+        for e in range(E):
+            n, k, at = n_len[e], k_len[e], slice(off[e], off[e + 1])
+            want, bound = reference(xs[src[at], :k], ws[e, :n, :k], None, wus[e, :n, :k] if gated else None, None,
+                                    "silu" if gated else "none", None, torch.finfo(dt).eps,
+                                    2.0 ** -20 if dtype == "f32" else 2.0 ** -18)
+            check(got[at, :n], want, bound)
+            assert (got[at, n:] == 0).all()
+
+
 def route_reference(logits, k, score, renorm, scale, keep, bias):
     """ids, weights, offsets, src, pos by definition, token by token."""
     T, E = logits.shape
