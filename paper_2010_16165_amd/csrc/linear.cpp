@@ -81,20 +81,22 @@ bool overlaps_weights(const fupr_matrix& y, const fupr_linear& op, const void* w
 // What a tile costs, in microseconds: `begin` from its first instruction to its first multiplication and from the last one
 // to its results, and `lo` or `hi` for 64 bytes of every row, `lo` where the workgroups leave room on the card, `hi`
 // where they fill it (each measured: layers of 256 to 4096 filters of 300 to 4096 weights on 16 to 8192 rows).
+// begun: what part of a row tile an expert's last one is taken to leave empty (the tallest skips an empty half).
 struct TileCost {
   int rows, cols, at_once;    // at_once: workgroups of a compute unit
+  float begun;
   float begin, lo, hi;        // 16-bit types
   float lo32, hi32;           // single precision; 0: not for it
 };
 constexpr TileCost kCosts[kLinearTiles] = {
-    {16, 16, 1, 0.7f, 0.055f, 0.055f, 0.055f, 0.055f},
-    {32, 32, 1, 2.0f, 0.045f, 0.060f, 0.085f, 0.095f},
-    {32, 64, 2, 2.2f, 0.070f, 0.132f, 0.14f, 0.26f},
-    {64, 64, 2, 2.8f, 0.118f, 0.25f, 0.27f, 0.52f},
-    {64, 128, 2, 4.0f, 0.19f, 0.48f, 0.48f, 0.92f},
-    {128, 128, 2, 4.8f, 0.32f, 0.62f, 0.93f, 1.9f},
-    {128, 256, 1, 6.0f, 0.29f, 0.42f, 0.f, 0.f},
-    {256, 256, 1, 8.7f, 0.54f, 0.72f, 0.f, 0.f},
+    {16, 16, 1, 0.6f, 1.0f, 0.050f, 0.050f, 0.050f, 0.050f},
+    {32, 32, 1, 0.6f, 2.6f, 0.045f, 0.060f, 0.085f, 0.095f},
+    {32, 64, 2, 0.6f, 2.4f, 0.070f, 0.145f, 0.14f, 0.26f},
+    {64, 64, 2, 0.6f, 2.8f, 0.118f, 0.25f, 0.27f, 0.52f},
+    {64, 128, 2, 0.6f, 4.0f, 0.19f, 0.48f, 0.48f, 0.92f},
+    {128, 128, 2, 0.6f, 4.8f, 0.32f, 0.62f, 0.93f, 1.9f},
+    {128, 256, 1, 0.6f, 6.0f, 0.29f, 0.42f, 0.f, 0.f},
+    {256, 256, 1, 0.4f, 8.7f, 0.54f, 0.72f, 0.f, 0.f},
 };
 
 // The kernel whose tiles are through first: small ones put more compute units to work, large ones read less for
@@ -116,16 +118,20 @@ LinearTile choose_tile(const LinearParams& p, fupr_dtype dt) {
     const int cols = p.w_up && t != kRows16x16 ? c.cols / 2 : c.cols;
     float rows = (float)((p.M - 1) / c.rows + 1);
     if (p.offsets) {
-      // the counts are on the device: as if every expert that can have rows left half a tile empty
-      const float begun = (float)(p.E < p.M ? p.E : p.M), about = (float)p.M / c.rows + 0.5f * begun;
+      // the counts are on the device: as if every expert that can have rows had some
+      const float begun = (float)(p.E < p.M ? p.E : p.M), about = (float)p.M / c.rows + c.begun * begun;
       rows = about > begun ? about : begun;
     }
     const float lo = (dt == FUPR_F32 ? c.lo32 : c.lo) * (p.w_up && t == kRows16x16 ? 1.6f : 1.f);
     const float hi = (dt == FUPR_F32 ? c.hi32 : c.hi) * (p.w_up && t == kRows16x16 ? 1.6f : 1.f);
+    // (finding a tile's expert and its rows of x takes time as well, where no weights are under way meanwhile)
+    const float begin = c.begin + (p.offsets && t != kRows16x16 ? 1.f : 0.f);
     const float fill = rows * (float)((p.N - 1) / cols + 1) / (float)(256 * c.at_once);
-    const float full = (float)(int)fill, rest = fill - full, more = rest > 0.5f ? 2.f * rest - 1.f : 0.f;
-    const float cost = full * (c.begin + units * hi) + (rest > 0.f ? c.begin + units * (lo + (hi - lo) * more) : 0.f) +
-                       (t == kRows16x16 ? 0.5f : 0.f);
+    const float full = (float)(int)fill, rest = fill - full;
+    // (where compute units take two, those that do set the pace; where one, it is the load on memory and power)
+    const float more = rest <= 0.5f ? 0.f : c.at_once > 1 ? 1.f : 2.f * rest - 1.f;
+    float cost = full * (begin + units * hi) + (rest > 0.f ? begin + units * (lo + (hi - lo) * more) : 0.f);
+    if (t == kRows16x16) cost = (fill > 1.f ? fill : 1.f) * (begin + units * lo);   // (many at a time: no rounds)
     if (which < 0 || cost < best) {
       best = cost;
       which = t;

@@ -6,6 +6,7 @@
 
 #include "device_utils.h"
 #include "linear.h"
+#include "wave_ops.h"
 
 namespace fupr {
 
@@ -112,62 +113,56 @@ __device__ __forceinline__ void with_activation(int act, F f) {
   }
 }
 
-// The row tiles of experts: which expert has tile `at`, and how many tiles there are.  Every lane returns the same.
-// A wave counts 64 experts at a time; an expert's rows are what its two offsets, clamped into 0 .. M, span.
+// The row tiles of experts: which expert has a tile, and how many tiles there are.  A wave counts 64 experts at a
+// time; an expert's rows are what its two offsets, clamped into 0 .. M, span.  All 64 lanes take part, and all return the same.
 struct ExpertRows {
   int e, lo, hi, tile;   // tile: of the expert's own
   int n_len, k_len;
 };
 template <int BM>
-__device__ __forceinline__ int expert_tiles(const LinearParams& p, int e, int& lo, int& hi) {
-  lo = hi = 0;
-  if (e < p.E) {
-    lo = min(max(p.offsets[e], 0), p.M);
-    hi = min(max(p.offsets[e + 1], lo), p.M);
+struct ExpertLanes {   // of the lane's expert
+  int lo = 0, hi = 0, n_len = 0, k_len = 0, tiles, upto;
+  __device__ __forceinline__ ExpertLanes(const LinearParams& p, int e) {
+    if (e < p.E) {
+      // (asked for together: one latency)
+      lo = min(max(p.offsets[e], 0), p.M);
+      hi = min(max(p.offsets[e + 1], lo), p.M);
+      n_len = p.n_len ? min(max(p.n_len[e], 0), p.N) : p.N;
+      k_len = p.k_len ? min(max(p.k_len[e], 0), p.K) : p.K;
+    }
+    tiles = (hi - lo + BM - 1) / BM;
+    upto = wave_prefix(tiles);
   }
-  return (hi - lo + BM - 1) / BM;
-}
-__device__ __forceinline__ int wave_prefix(int v, int lane) {   // inclusive
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
-}
-template <int BM>
-__device__ __forceinline__ int count_expert_tiles(const LinearParams& p, int lane) {
-  int total = 0;
-  for (int e0 = 0; e0 < p.E; e0 += 64) {
-    int lo, hi;
-    total += __shfl(wave_prefix(expert_tiles<BM>(p, e0 + lane, lo, hi), lane), 63);
-  }
-  return __builtin_amdgcn_readfirstlane(total);
-}
-template <int BM>
-__device__ __forceinline__ bool find_expert(const LinearParams& p, int at, int lane, ExpertRows& out) {
+  __device__ __forceinline__ int all() const { return __builtin_amdgcn_readlane(upto, 63); }
+};
+// pick(tiles of all experts) says which of them is looked for, or -1.  COUNTS: pick looks at their number.
+template <int BM, bool COUNTS, class Pick>
+__device__ __forceinline__ bool find_expert(const LinearParams& p, int lane, Pick pick, ExpertRows& out) {
+  ExpertLanes<BM> x(p, lane);
+  int total = x.all();
+  if (COUNTS)
+    for (int e0 = 64; e0 < p.E; e0 += 64) total += ExpertLanes<BM>(p, e0 + lane).all();
+  const int at = pick(total);
+  if (at < 0) return false;
   int before = 0;
-  for (int e0 = 0; e0 < p.E; e0 += 64) {
-    int lo, hi;
-    const int n = expert_tiles<BM>(p, e0 + lane, lo, hi);
-    // (asked for together with the offsets: one latency, not two)
-    const int mine_n = p.n_len && e0 + lane < p.E ? p.n_len[e0 + lane] : p.N;
-    const int mine_k = p.k_len && e0 + lane < p.E ? p.k_len[e0 + lane] : p.K;
-    const int upto = before + wave_prefix(n, lane);
-    const uint64_t mine = __ballot(at >= upto - n && at < upto);
+  for (int e0 = 0;;) {
+    const int upto = before + x.upto;
+    const uint64_t mine = __ballot(at >= upto - x.tiles && at < upto);
     if (mine) {
       const int who = __builtin_ctzll(mine);
-      out.e = __builtin_amdgcn_readfirstlane(e0 + who);
-      out.lo = __builtin_amdgcn_readfirstlane(__shfl(lo, who));
-      out.hi = __builtin_amdgcn_readfirstlane(__shfl(hi, who));
-      out.tile = __builtin_amdgcn_readfirstlane(at - __shfl(upto - n, who));
-      out.n_len = __builtin_amdgcn_readfirstlane(min(max(__shfl(mine_n, who), 0), p.N));
-      out.k_len = __builtin_amdgcn_readfirstlane(min(max(__shfl(mine_k, who), 0), p.K));
+      out.e = e0 + who;
+      out.lo = __builtin_amdgcn_readlane(x.lo, who);
+      out.hi = __builtin_amdgcn_readlane(x.hi, who);
+      out.tile = at - __builtin_amdgcn_readlane(upto - x.tiles, who);
+      out.n_len = __builtin_amdgcn_readlane(x.n_len, who);
+      out.k_len = __builtin_amdgcn_readlane(x.k_len, who);
       return true;
     }
-    before = __shfl(upto, 63);
+    before += x.all();
+    e0 += 64;
+    if (e0 >= p.E) return false;
+    x = ExpertLanes<BM>(p, e0 + lane);
   }
-  return false;
 }
 
 // Workgroups go to the eight XCDs in turn; tile numbers are handed out so that an XCD takes a contiguous range of
@@ -178,53 +173,56 @@ __device__ __forceinline__ int tile_of_workgroup(int id, int total) {
   return (id >> 3) < each && at < total ? at : -1;
 }
 
-// COUNT consecutive results (4 or 8) of one row from column n on: + res, one rounding, stored with 16-byte accesses
-// where the row still has that many columns.
-template <int TY, int COUNT>
-__device__ __forceinline__ void store_run(const LinearParams& p, int64_t row, int n, float* v) {
+// What is added to four consecutive results of one row from column n on, in its own type (16 bits: in two words).  Whole
+// pieces are read, also of a row that ends inside one: a row's memory extends to its stride.
+template <int TY>
+__device__ __forceinline__ uint4 load_four(const LinearParams& p, int64_t row, int n) {
+  uint4 r = {0u, 0u, 0u, 0u};
+  if (p.res && n < p.N) {
+    const char* res = p.res + row * p.res_stride;
+    if (TY == FUPR_F32 || p.y_f32) {
+      r = *reinterpret_cast<const uint4*>(res + (int64_t)n * 4);
+    } else {
+      const uint2 q = *reinterpret_cast<const uint2*>(res + (int64_t)n * 2);
+      r.x = q.x;
+      r.y = q.y;
+    }
+  }
+  return r;
+}
+// Four consecutive results of one row from column n on: + res, one rounding, one store where the row still has four.
+template <int TY>
+__device__ __forceinline__ void store_four(const LinearParams& p, int64_t row, int n, float (&v)[4], const uint4& add) {
   if (n >= p.N) return;
-  const bool whole = n + COUNT <= p.N;
-  const int es = TY == FUPR_F32 || p.y_f32 ? 4 : 2;
-  char* y = p.y + row * p.y_stride + (int64_t)n * es;
-  const char* res = p.res ? p.res + row * p.res_stride + (int64_t)n * es : nullptr;
+  const bool whole = n + 4 <= p.N;
+  char* const to = p.y + row * p.y_stride;
   if (TY == FUPR_F32 || p.y_f32) {
-    if (whole) {
+    float* y = reinterpret_cast<float*>(to) + n;
+    const uint32_t d[4] = {add.x, add.y, add.z, add.w};
+    if (p.res) {
 #pragma unroll
-      for (int i = 0; i < COUNT; i += 4) {
-        f32x4 r = {0.f, 0.f, 0.f, 0.f};
-        if (res) r = *reinterpret_cast<const f32x4*>(res + i * 4);
-        *reinterpret_cast<f32x4*>(y + i * 4) = f32x4{v[i] + r[0], v[i + 1] + r[1], v[i + 2] + r[2], v[i + 3] + r[3]};
-      }
+      for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(d[i]);
+    }
+    if (whole) {
+      *reinterpret_cast<f32x4*>(y) = f32x4{v[0], v[1], v[2], v[3]};
     } else {
 #pragma unroll
-      for (int i = 0; i < COUNT; ++i)
-        if (n + i < p.N)
-          reinterpret_cast<float*>(y)[i] = v[i] + (res ? reinterpret_cast<const float*>(res)[i] : 0.f);
+      for (int i = 0; i < 4; ++i)
+        if (n + i < p.N) y[i] = v[i];
     }
   } else {
     constexpr bool BF = TY == FUPR_BF16;
+    uint16_t* y = reinterpret_cast<uint16_t*>(to) + n;
+    if (p.res) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] += to_float<BF>((uint16_t)((i < 2 ? add.x : add.y) >> (i & 1) * 16));
+    }
     if (whole) {
-      uint32_t r[COUNT / 2] = {}, o[COUNT / 2];
-      if (res) {
-#pragma unroll
-        for (int i = 0; i < COUNT / 4; ++i) {
-          const uint2 q = *reinterpret_cast<const uint2*>(res + i * 8);
-          r[2 * i] = q.x;
-          r[2 * i + 1] = q.y;
-        }
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] += to_float<BF>((uint16_t)(r[i / 2] >> (i & 1) * 16));
-      }
-#pragma unroll
-      for (int i = 0; i < COUNT / 2; ++i) o[i] = pack2<BF>(v[2 * i], v[2 * i + 1]);
-      if constexpr (COUNT == 8) *reinterpret_cast<uint4*>(y) = uint4{o[0], o[1], o[2], o[3]};
-      else *reinterpret_cast<uint2*>(y) = uint2{o[0], o[1]};
+      *reinterpret_cast<uint2*>(y) = uint2{pack2<BF>(v[0], v[1]), pack2<BF>(v[2], v[3])};
     } else {
 #pragma unroll
-      for (int i = 0; i < COUNT; ++i)
-        if (n + i < p.N)
-          reinterpret_cast<uint16_t*>(y)[i] =
-              from_float<BF>(v[i] + (res ? to_float<BF>(reinterpret_cast<const uint16_t*>(res)[i]) : 0.f));
+      for (int i = 0; i < 4; ++i)
+        if (n + i < p.N) y[i] = from_float<BF>(v[i]);
     }
   }
 }

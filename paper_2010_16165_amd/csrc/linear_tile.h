@@ -28,12 +28,15 @@ struct TilePlace {
 template <int BM>
 __device__ __forceinline__ bool find_tile(const LinearParams& p, int lane, TilePlace& t) {
   if (p.offsets) {
-    const int at = tile_of_workgroup(blockIdx.x, count_expert_tiles<BM>(p, lane) * p.n_tiles);
-    if (at < 0) return false;
     ExpertRows r;
-    const int mt = at / p.n_tiles;
-    if (!find_expert<BM>(p, mt, lane, r)) return false;
-    t = TilePlace{r.e, r.hi, r.lo + r.tile * BM, at - mt * p.n_tiles, r.n_len, r.k_len};
+    int nt = 0;
+    auto pick = [&](int tiles) {
+      const int at = tile_of_workgroup(blockIdx.x, tiles * p.n_tiles), mt = at / p.n_tiles;
+      nt = at - mt * p.n_tiles;
+      return at < 0 ? -1 : mt;
+    };
+    if (!find_expert<BM, true>(p, lane, pick, r)) return false;
+    t = TilePlace{r.e, r.hi, r.lo + r.tile * BM, nt, r.n_len, r.k_len};
     return true;
   }
   // strips of eight row tiles: what an XCD holds at one time is about as tall as it is wide
@@ -111,24 +114,49 @@ __device__ __forceinline__ void store_row(const LinearParams& p, int64_t row, in
 // What stands between a wave's sums and y: bias, activation, gate, residual, rounding.  The sums come from the wave's
 // own part of LDS, where eight consecutive columns of a row meet in a lane and the work is a loop that is not written
 // out for every register: a version straight from the registers spilled them and took 10 us more for a tile of
-// 256 x 256.  `rows` rows of CHUNKS chunks of four columns (gated: the gate's half, then the other's), chunk c at
-// c ^ (row modulo CHUNKS).  first: the row of y, nb: the column where they begin.
-template <int TY, int CHUNKS, int KS, bool GATED>
-__device__ __forceinline__ void finish_rows(const LinearParams& p, const char* lds, int apart, int from_row, int rows, int e, int hi, int first, int nb,
-                                            int n_len, int lane) {
-  constexpr bool FINE = TY == FUPR_F32;
-  constexpr int kCols = GATED ? CHUNKS * 2 : CHUNKS * 4, kLanes = kCols / 8;   // of a row
-  const int c = lane % kLanes, n = nb + c * 8;
+// 256 x 256.
+//
+// What is added to rows from_row .. rows of the wave's part is asked for two turns ahead, the first two here: small tiles
+// call this before their first multiplication.  first: the row of y that row 0 is, nb: the column where they begin.
+template <int TY>
+struct FinishInputs {
   float bias[8], up[8];
+  Addend<TY> next, after;
+};
+template <int NT>
+__device__ __forceinline__ constexpr int finish_lanes(bool gated) {   // of a row
+  return gated ? NT : NT * 2;
+}
+template <int TY, int NT>
+__device__ __forceinline__ FinishInputs<TY> ask_finish(const LinearParams& p, bool gated, int from_row, int rows, int e, int hi,
+                                                       int first, int nb, int n_len, int lane) {
+  const int lanes = finish_lanes<NT>(gated), turn = 64 / lanes;
+  const int n = nb + lane % lanes * 8;
+  FinishInputs<TY> in;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    bias[i] = p.bias && n + i < n_len ? p.bias[(int64_t)e * p.N + n + i] : 0.f;
-    up[i] = GATED && p.bias_up && n + i < n_len ? p.bias_up[(int64_t)e * p.N + n + i] : 0.f;
+    in.bias[i] = p.bias && n + i < n_len ? p.bias[(int64_t)e * p.N + n + i] : 0.f;
+    in.up[i] = p.bias_up && n + i < n_len ? p.bias_up[(int64_t)e * p.N + n + i] : 0.f;
   }
+  const int r = from_row + lane / lanes;
+  in.next = load_addend<TY>(p, first + r, n, r < rows && first + r < hi);
+  in.after = load_addend<TY>(p, first + r + turn, n, r + turn < rows && first + r + turn < hi);
+  return in;
+}
+// Rows of NT * 4 chunks of four columns (gated: the gate's half, then the other's), chunk c at c ^ (row modulo chunks), in
+// KS copies `apart` bytes from each other, whose sum is the result.
+template <int TY, int NT, int KS, bool GATED>
+__device__ __forceinline__ void finish_rows(const LinearParams& p, FinishInputs<TY> in, const char* lds, int apart, int from_row,
+                                            int rows, int hi, int first, int nb, int n_len, int lane) {
+  constexpr bool FINE = TY == FUPR_F32;
+  constexpr int CHUNKS = NT * 4, kLanes = finish_lanes<NT>(GATED), kTurn = 64 / kLanes;
+  const int c = lane % kLanes, n = nb + c * 8;
 #pragma unroll 1
-  for (int r = from_row + lane / kLanes; r < rows; r += 64 / kLanes) {
-    const int row = first + r;
-    const Addend<TY> add = load_addend<TY>(p, row, n, row < hi);
+  for (int r = from_row + lane / kLanes; r < rows; r += kTurn) {
+    const int row = first + r, later = r + 2 * kTurn;
+    const Addend<TY> add = in.next;
+    in.next = in.after;
+    in.after = load_addend<TY>(p, first + later, n, later < rows && first + later < hi);
     const char* from = lds + r * CHUNKS * 16;
     float v[8], u[8];
 #pragma unroll
@@ -143,8 +171,8 @@ __device__ __forceinline__ void finish_rows(const LinearParams& p, const char* l
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        v[q * 4 + i] = a[i] + bias[q * 4 + i];
-        u[q * 4 + i] = b[i] + up[q * 4 + i];
+        v[q * 4 + i] = a[i] + in.bias[q * 4 + i];
+        u[q * 4 + i] = b[i] + in.up[q * 4 + i];
       }
     }
     with_activation(p.act, [&](auto act) {
@@ -160,26 +188,43 @@ __device__ __forceinline__ void finish_rows(const LinearParams& p, const char* l
   }
 }
 
-// From a wave's accumulators of 16 x 16 tiles to y, EM row tiles at a time.
-template <int TY, int MT, int NT, int EM, int KS, bool GATED>
-__device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4 (&acc)[MT][NT], char* lds, int apart,
-                                              int group, int e, int hi, int row0, int nb, int n_len, int lane) {
+// A wave's accumulators of EM x NT tiles of 16 x 16 to LDS, as finish_rows reads them.
+template <int MT, int NT, int EM, bool GATED>
+__device__ __forceinline__ void stage_tiles(const f32x4 (&acc)[MT][NT], int begin, char* lds, int lane) {
   constexpr int kChunks = NT * 4;
-  static_assert(MT % EM == 0 && (KS == 1 || EM == MT) && EM * 16 % KS == 0, "whole parts");
-  char* const own = lds + group * apart;
+#pragma unroll
+  for (int i = 0; i < EM; ++i)
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int r = lane & 15, g = lane >> 4;
+      const int at = GATED ? (t & 1) * (kChunks / 2) + g * (NT / 2) + t / 2 : g * NT + t;
+      *reinterpret_cast<f32x4*>(lds + (i * 16 + r) * kChunks * 16 + ((at ^ r) & (kChunks - 1)) * 16) = acc[begin + i][t];
+    }
+}
+
+// From a wave's accumulators to y, EM row tiles at a time.
+template <int TY, int MT, int NT, int EM, bool GATED>
+__device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4 (&acc)[MT][NT], char* lds, int e, int hi,
+                                              int row0, int nb, int n_len, int lane) {
+  static_assert(MT % EM == 0, "whole parts");
 #pragma unroll
   for (int part = 0; part < MT / EM; ++part) {
-#pragma unroll
-    for (int i = 0; i < EM; ++i)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const int r = lane & 15, g = lane >> 4;
-        const int at = GATED ? (t & 1) * (kChunks / 2) + g * (NT / 2) + t / 2 : g * NT + t;
-        *reinterpret_cast<f32x4*>(own + (i * 16 + r) * kChunks * 16 + ((at ^ r) & (kChunks - 1)) * 16) = acc[part * EM + i][t];
-      }
-    if constexpr (KS > 1) __syncthreads();
-    finish_rows<TY, kChunks, KS, GATED>(p, lds, apart, group * (EM * 16 / KS), (group + 1) * (EM * 16 / KS), e, hi, row0 + part * EM * 16, nb, n_len, lane);
+    const int first = row0 + part * EM * 16;
+    const FinishInputs<TY> in = ask_finish<TY, NT>(p, GATED, 0, EM * 16, e, hi, first, nb, n_len, lane);
+    stage_tiles<MT, NT, EM, GATED>(acc, part * EM, lds, lane);
+    finish_rows<TY, NT, 1, GATED>(p, in, lds, 0, 0, EM * 16, hi, first, nb, n_len, lane);
   }
+}
+
+// The same of tiles whose reduction KS groups of waves share, `apart` bytes of LDS each: a group finishes a part of the rows.
+template <int TY, int MT, int NT, int KS, bool GATED>
+__device__ __forceinline__ void shared_epilogue(const LinearParams& p, const FinishInputs<TY>& in, const f32x4 (&acc)[MT][NT], char* lds,
+                                                int apart, int group, int hi, int row0, int nb, int n_len, int lane) {
+  constexpr int kRows = MT * 16 / KS;
+  static_assert(MT * 16 % KS == 0, "whole rows");
+  stage_tiles<MT, NT, MT, GATED>(acc, 0, lds + group * apart, lane);
+  if constexpr (KS > 1) __syncthreads();
+  finish_rows<TY, NT, KS, GATED>(p, in, lds, apart, group * kRows, (group + 1) * kRows, hi, row0, nb, n_len, lane);
 }
 
 // Tiles of a launch, as a multiple of eight (workgroups go to the eight XCDs in turn); false: more than a grid holds.

@@ -72,6 +72,14 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * 1024;
 
+  const int wm = wave / G::WN, wn = wave % G::WN;
+  const int row0 = m0 + wm * MT * 16, nb = n0 + wn * NT * (gated ? 8 : 16);
+  // small tiles have registers to ask for what the epilogue adds before they begin
+  constexpr bool kEarly = MT * NT <= 4;
+  FinishInputs<G::TY> in;
+  if constexpr (kEarly)
+    in = ask_finish<G::TY, NT>(p, gated, group * (MT * 16 / KS), (group + 1) * (MT * 16 / KS), e, hi, row0, nb, n_len, lane);
+
   // One load of unit `issued`, into buffer `to`.  In the unit that the reduction ends in, chunks behind its last one are
   // that last one again (inside the row, and zeroed below).
   int issued = 0, to = 0;
@@ -111,7 +119,6 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = zero;
 
-  const int wm = wave / G::WN, wn = wave % G::WN;
   constexpr int kTwice = G::twice, kOnce = MT - kTwice;
   uint4 a[2][NT], b[kOnce > 0 ? kOnce : 1], c[2][kTwice];   // c: the last kTwice rows' operands
   const char* const ws = lds + BM * 64 + wn * NT * 1024 + (lane & 15) * 64 + ((lane >> 4) ^ (lane >> 1 & 3)) * 16;
@@ -199,14 +206,20 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
     for (; u < units; u += kTurns) turns(std::false_type{}, u);
   }
 
-  const int row0 = m0 + wm * MT * 16;
   __syncthreads();   // (no wave reads operands any more)
   constexpr int kMine = 16 * NT * 64;   // bytes of a row tile of accumulators
-  constexpr int EM = G::waves * MT * kMine <= D * G::buf ? MT : G::waves * MT * kMine <= 2 * D * G::buf ? MT / 2 : MT / 4;
-  constexpr int apart = D * G::buf;
-  char* mine = lds_all + wave * EM * kMine;
-  if (gated) tile_epilogue<G::TY, MT, NT, EM, KS, true>(p, acc, mine, apart, group, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
-  else tile_epilogue<G::TY, MT, NT, EM, KS, false>(p, acc, mine, apart, group, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
+  if constexpr (kEarly) {
+    static_assert(G::waves * MT * kMine <= D * G::buf, "a group's sums in its buffers");
+    char* mine = lds_all + wave * MT * kMine;
+    if (gated) shared_epilogue<G::TY, MT, NT, KS, true>(p, in, acc, mine, D * G::buf, group, hi, row0, nb, n_len, lane);
+    else shared_epilogue<G::TY, MT, NT, KS, false>(p, in, acc, mine, D * G::buf, group, hi, row0, nb, n_len, lane);
+  } else {
+    constexpr int EM = G::waves * MT * kMine <= D * G::buf ? MT : MT / 2;
+    static_assert(KS == 1 && G::waves * EM * kMine <= D * G::buf, "sums in the buffers");
+    char* mine = lds_all + wave * EM * kMine;
+    if (gated) tile_epilogue<G::TY, MT, NT, EM, true>(p, acc, mine, e, hi, row0, nb, n_len, lane);
+    else tile_epilogue<G::TY, MT, NT, EM, false>(p, acc, mine, e, hi, row0, nb, n_len, lane);
+  }
 }
 
 template <class G>

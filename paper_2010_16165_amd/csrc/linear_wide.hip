@@ -166,6 +166,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
 
   if (steps > 0) {
     const bool late = wm != 0;
+    const bool alive = m0 + wm * MT * 16 < hi;   // (a half without a row of its own only loads)
 #pragma unroll 1
     for (int d = 0; d < 2 && d < steps; ++d) {
       ask_w();
@@ -187,24 +188,29 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
     // memory every few instructions, 2 us per KB)
     int s = 0;
     for (; s < steps - 2; ++s) {
-      read();
+      if (alive) read();
       ask_w();                  // of step s + 2
       wait_loads<kLoads>();     // filters of step s + 1 have landed
       phase_ends();
       begin_x();                // of step s + 2
-      multiply(std::true_type{});
+      if (alive) {
+        multiply(std::true_type{});
+      } else {
+#pragma unroll
+        for (int i = 0; i < kXLoads; ++i) load_x(i);
+      }
       end_x();
       wait_loads<kLoads>();     // rows of step s + 1
       phase_ends();
     }
     for (; s < steps; ++s) {
-      read();
+      if (alive) read();
       if (s + 1 < steps) {
         wait_loads<kXLoads>();
         clear_w();
       }
       phase_ends();
-      multiply(std::false_type{});
+      if (alive) multiply(std::false_type{});
       if (s + 1 < steps) {
         wait_loads<0>();
         clear_x();
@@ -218,8 +224,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void linear_wide_kernel(LinearParam
   constexpr int EM = 4;
   static_assert(kWaves * EM * 16 * NT * 64 <= sizeof(lds), "four row tiles of every wave");
   char* mine = lds + wave * EM * 16 * NT * 64;
-  if (gated) tile_epilogue<TY, MT, NT, EM, 1, true>(p, acc, mine, 0, 0, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
-  else tile_epilogue<TY, MT, NT, EM, 1, false>(p, acc, mine, 0, 0, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
+  if (gated) tile_epilogue<TY, MT, NT, EM, true>(p, acc, mine, e, hi, row0, n0 + wn * NT * 8, n_len, lane);
+  else tile_epilogue<TY, MT, NT, EM, false>(p, acc, mine, e, hi, row0, n0 + wn * NT * 16, n_len, lane);
 }
 
 }  // namespace

@@ -15,6 +15,7 @@
 
 #include "device_utils.h"
 #include "linear.h"
+#include "wave_ops.h"
 
 namespace fupr {
 
@@ -23,7 +24,10 @@ fupr_status launch_status(const char* what);
 namespace {
 
 constexpr int kMostExperts = 1024, kMostChosen = 16;
-constexpr int kOneTokens = 256;     // up to here one workgroup chooses and orders, in one launch
+constexpr int kMostWaves = 16;      // of a workgroup that chooses
+// Up to here one workgroup chooses and orders, in one launch: 64 tokens of 128 experts 9 - 14 us against 13 - 18 us by
+// two launches, 256 tokens 28 - 46 us.
+constexpr int kOneTokens = 64;
 constexpr int kManyBlocks = 256;    // from here on workgroups take more than 64 tokens each
 constexpr int kWhoBytes = 48 << 10; // of LDS, for the words that say who chose an expert
 
@@ -62,24 +66,59 @@ __device__ __forceinline__ uint64_t key_of(double v) {
   return b >> 63 ? ~b : b | 1ull << 63;
 }
 
-template <int LPT>
-__device__ __forceinline__ float group_max(float v) {
-#pragma unroll
-  for (int d = 1; d < LPT; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+template <int LPT, class T>
+__device__ __forceinline__ T group_sum(T v) {
+  return group_fold<LPT>(v, [](T a, T b) { return a + b; });
 }
-template <int LPT, class F>
-__device__ __forceinline__ F group_sum(F v) {
-#pragma unroll
-  for (int d = 1; d < LPT; d *= 2) v += __shfl_xor(v, d);
-  return v;
+
+// e^x in fp64 for x <= 0: x = n ln 2 + r, |r| <= ln 2 / 2, and the Taylor polynomial of degree 13 (the next term is
+// 4e-18).  A NaN stays one.
+__device__ __forceinline__ double exp_below(double x) {
+  x = x < -800.0 ? -800.0 : x;
+  const double n = __builtin_rint(x * 1.4426950408889634);
+  const double r = __builtin_fma(n, -2.3190468138462996e-17, __builtin_fma(n, -0.69314718055994529, x));
+  double v = 1.0 / 6227020800.0;
+  v = __builtin_fma(v, r, 1.0 / 479001600.0);
+  v = __builtin_fma(v, r, 1.0 / 39916800.0);
+  v = __builtin_fma(v, r, 1.0 / 3628800.0);
+  v = __builtin_fma(v, r, 1.0 / 362880.0);
+  v = __builtin_fma(v, r, 1.0 / 40320.0);
+  v = __builtin_fma(v, r, 1.0 / 5040.0);
+  v = __builtin_fma(v, r, 1.0 / 720.0);
+  v = __builtin_fma(v, r, 1.0 / 120.0);
+  v = __builtin_fma(v, r, 1.0 / 24.0);
+  v = __builtin_fma(v, r, 1.0 / 6.0);
+  v = __builtin_fma(v, r, 0.5);
+  v = __builtin_fma(v, r, 1.0);
+  v = __builtin_fma(v, r, 1.0);
+  return __builtin_ldexp(v, (int)n);
+}
+// 1 / d for 1 <= d <= 2048: two Newton steps from the hardware's first bits
+__device__ __forceinline__ double one_over(double d) {
+  double r = __builtin_amdgcn_rcp(d);
+  r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+  return __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+}
+
+// The largest key of a group of LPT lanes and its expert, of equal ones the lowest.
+template <int LPT, int D = 1>
+__device__ __forceinline__ void fold_best(uint64_t& key, uint32_t& at) {
+  if constexpr (D < LPT) {
+    const uint64_t other = fold_partner<D>(key);
+    const uint32_t there = fold_partner<D>(at);
+    if (other > key || (other == key && there < at)) {
+      key = other;
+      at = there;
+    }
+    fold_best<LPT, D * 2>(key, at);
+  }
 }
 
 // The chosen experts of one token by a group of LPT lanes; lane j < k of the group returns the j-th (or -1) and its
 // weight.
 template <int LPT, int V, bool BIASED>
 __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int sub, int& id, float& weight) {
-  typedef typename std::conditional<BIASED, unsigned long long, uint32_t>::type Key;
+  typedef typename std::conditional<BIASED, uint64_t, uint32_t>::type Key;
   float l[V];
   Key key[V];
 #pragma unroll
@@ -92,51 +131,61 @@ __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int 
   if (!p.sigmoid) {
 #pragma unroll
     for (int i = 0; i < V; ++i) most = fmaxf(most, l[i]);
-    most = group_max<LPT>(most);
+    most = group_fold<LPT>(most, [](float a, float b) { return fmaxf(a, b); });
     if (most == -__builtin_inff()) most = 0.f;   // no expert at all
-#pragma unroll
-    for (int i = 0; i < V; ++i) sum += expf(l[i] - most);
-    sum = group_sum<LPT>(sum);
   }
   if constexpr (BIASED) {
-    double wide[V], total = 0.0;
+    double wide[V];
+    if (p.sigmoid) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      wide[i] = p.sigmoid ? 1.0 / (1.0 + exp(-(double)l[i])) : exp((double)l[i] - (double)most);
-      total += wide[i];
+      for (int i = 0; i < V; ++i) {
+        const double t = exp_below(-__builtin_fabs((double)l[i])), r = one_over(1.0 + t);
+        wide[i] = l[i] < 0.f ? t * r : r;   // (of a NaN: NaN)
+      }
+    } else {
+      double total = 0.0;
+#pragma unroll
+      for (int i = 0; i < V; ++i) total += wide[i] = exp_below((double)l[i] - (double)most);
+      total = group_sum<LPT>(total);
+      sum = (float)total;
+      const double r = one_over(total);
+#pragma unroll
+      for (int i = 0; i < V; ++i) wide[i] *= r;
     }
-    if (p.sigmoid) total = 1.0;
-    else total = group_sum<LPT>(total);
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      key[i] = l[i] == -__builtin_inff() ? 0 : key_of(wide[i] / total + (double)p.bias[min(i * LPT + sub, p.E - 1)]);
+      key[i] = l[i] == -__builtin_inff() ? 0 : key_of(wide[i] + (double)p.bias[min(i * LPT + sub, p.E - 1)]);
   } else {
+    if (!p.sigmoid) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum += expf(l[i] - most);
+      sum = group_sum<LPT>(sum);
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) key[i] = key_of(l[i]);
   }
   id = -1;
   for (int j = 0; j < p.k; ++j) {
     Key best = 0;
-    int at = 0;
+    uint32_t at = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i)
       if (key[i] > best) {   // (ascending experts: the first of equals stays)
         best = key[i];
         at = i * LPT + sub;
       }
-#pragma unroll
-    for (int d = 1; d < LPT; d *= 2) {
-      const Key other = __shfl_xor(best, d);
-      const int there = __shfl_xor(at, d);
-      if (other > best || (other == best && there < at)) {
-        best = other;
-        at = there;
-      }
+    if constexpr (BIASED) {
+      fold_best<LPT>(best, at);
+    } else {
+      // one number: of equal keys the lower expert's is the larger
+      const uint64_t both = group_fold<LPT>((uint64_t)best << 32 | (uint32_t)~at, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+      best = (uint32_t)(both >> 32);
+      at = ~(uint32_t)both;
     }
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (i * LPT + sub == at) key[i] = 0;
-    if (sub == j % LPT && best != 0) id = at;
+      if (i * LPT + sub == (int)at) key[i] = 0;
+    if (sub == j % LPT && best != 0) id = (int)at;
   }
   float score = 0.f;
   if (id >= 0) {
@@ -188,14 +237,9 @@ __device__ __forceinline__ void prefix_experts(int E, const int* counts, int* fi
     int before = 0;
     for (int e0 = 0; e0 < E; e0 += 64) {
       const int e = e0 + threadIdx.x, own = e < E ? counts[e] : 0;
-      int v = own;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int o = __shfl_up(v, d);
-        if ((int)threadIdx.x >= d) v += o;
-      }
+      const int v = wave_prefix(own);
       if (e < E) first[e] = before + v - own;
-      before += __shfl(v, 63);
+      before += __builtin_amdgcn_readlane(v, 63);
     }
     if (threadIdx.x == 0) first[E] = before;
   }
@@ -204,7 +248,7 @@ __device__ __forceinline__ void prefix_experts(int E, const int* counts, int* fi
 
 // ONE: the only workgroup, so the rows are ordered at once.
 template <int LPT, int V, bool BIASED, bool ONE>
-__global__ __launch_bounds__(512) void route_choose_kernel(RouteParams p) {
+__global__ __launch_bounds__(kMostWaves * 64) void route_choose_kernel(RouteParams p) {
   constexpr int kPer = 64 / LPT;
   const RouteLds l = route_lds(p);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, sub = lane % LPT;
@@ -284,7 +328,7 @@ __global__ __launch_bounds__(1024) void route_place_kernel(RouteParams p) {
 template <int LPT, int V, bool BIASED>
 void launch_route_as(const RouteParams& p, hipStream_t st) {
   const int tokens = std::min(p.T, p.groups * 64);
-  const int waves = std::min(8, (tokens * LPT + 63) / 64);
+  const int waves = std::min(kMostWaves, (tokens * LPT + 63) / 64);
   if (p.blocks == 1) {
     route_choose_kernel<LPT, V, BIASED, true><<<dim3(1), dim3(waves * 64), route_lds_bytes(p, true), st>>>(p);
   } else {
@@ -434,9 +478,9 @@ fupr_status fupr_moe_route(const fupr_router* router, const fupr_matrix* logits,
   p.groups = route_groups(p.T, p.E);
   p.blocks = route_blocks(p.T, p.E);
   hipStream_t s = (hipStream_t)stream;
-  // the fewest lanes that hold a token's logits in 16 registers each, and one for every expert chosen
-  if (p.E <= 64 && p.k <= 8) launch_route<8, 8>(p, s);
-  else if (p.E <= 128 && p.k <= 8) launch_route<8, 16>(p, s);
+  // sixteen lanes: one for every expert chosen, few logits to look through in each; more where 16 registers are not enough
+  if (p.E <= 64) launch_route<16, 4>(p, s);
+  else if (p.E <= 128) launch_route<16, 8>(p, s);
   else if (p.E <= 256) launch_route<16, 16>(p, s);
   else if (p.E <= 512) launch_route<32, 16>(p, s);
   else launch_route<64, 16>(p, s);
