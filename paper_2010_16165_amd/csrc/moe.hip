@@ -2,8 +2,8 @@
 //
 // Choosing: a group of LPT lanes has one token, each lane V of its logits in registers; top_k times the group takes
 // the largest key among its lanes (ties: lowest expert) and strikes it out.  Keys are the logits themselves where no
-// bias is added - softmax and sigmoid are monotonic, so no rounding of theirs decides - and score + bias in fp64 where
-// one is, because two scores may lie closer than fp32 tells apart.
+// bias is added - softmax and sigmoid are monotonic, so no rounding of theirs decides.  Where one is, they are score +
+// bias in fp32 with the error that they may have, and in fp64 where that leaves two of the largest too close to tell apart.
 //
 // Ordering rows by expert, then token: for 64 tokens and an expert one 64-bit word says which of them chose it (atomic
 // OR in LDS: no order of arrival shows in it), so a slot's place is a count of bits below its own.
@@ -114,17 +114,62 @@ __device__ __forceinline__ void fold_best(uint64_t& key, uint32_t& at) {
   }
 }
 
-// The chosen experts of one token by a group of LPT lanes; lane j < k of the group returns the j-th (or -1) and its
-// weight.
+__device__ __forceinline__ float value_of(uint32_t key) {   // of which key_of made it; of all ones a NaN
+  return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
+// The experts of the `rounds` largest keys: lane j of the group gets the j-th in id.  each(j, key) is told the largest key
+// of every round.  keys are struck out.
+template <int LPT, int V, class Each>
+__device__ __forceinline__ void choose_by_32(uint32_t (&key)[V], int rounds, int sub, int& id, Each each) {
+  for (int j = 0; j < rounds; ++j) {
+    uint32_t best = 0, at = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (key[i] > best) {   // (ascending experts: the first of equals stays)
+        best = key[i];
+        at = i * LPT + sub;
+      }
+    // one number: of equal keys the lower expert's is the larger
+    const uint64_t both = group_fold<LPT>((uint64_t)best << 32 | (uint32_t)~at, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
+    best = (uint32_t)(both >> 32);
+    at = ~(uint32_t)both;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i * LPT + sub == (int)at) key[i] = 0;
+    if (sub == j && best != 0) id = (int)at;
+    each(j, best);
+  }
+}
+template <int LPT, int V>
+__device__ __forceinline__ void choose_by_64(uint64_t (&key)[V], int k, int sub, int& id) {
+  for (int j = 0; j < k; ++j) {
+    uint64_t best = 0;
+    uint32_t at = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (key[i] > best) {
+        best = key[i];
+        at = i * LPT + sub;
+      }
+    fold_best<LPT>(best, at);
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i * LPT + sub == (int)at) key[i] = 0;
+    if (sub == j && best != 0) id = (int)at;
+  }
+}
+
+// The chosen experts of one token by a group of LPT lanes (of at least k); lane j < k of the group returns the j-th (or
+// -1) and its weight.
 template <int LPT, int V, bool BIASED>
 __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int sub, int& id, float& weight) {
-  typedef typename std::conditional<BIASED, uint64_t, uint32_t>::type Key;
-  float l[V];
-  Key key[V];
+  float l[V], e[V];
+  uint32_t key[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    const int e = i * LPT + sub;
-    l[i] = e < p.E && !(p.keep && p.keep[e] == 0) ? logit_at(p, token, e) : -__builtin_inff();
+    const int at = i * LPT + sub;
+    l[i] = at < p.E && !(p.keep && p.keep[at] == 0) ? logit_at(p, token, at) : -__builtin_inff();
   }
   // softmax: the largest logit and the sum of exponentials (an expert that does not exist has e^-inf = 0)
   float most = -__builtin_inff(), sum = 0.f;
@@ -133,59 +178,83 @@ __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int 
     for (int i = 0; i < V; ++i) most = fmaxf(most, l[i]);
     most = group_fold<LPT>(most, [](float a, float b) { return fmaxf(a, b); });
     if (most == -__builtin_inff()) most = 0.f;   // no expert at all
-  }
-  if constexpr (BIASED) {
-    double wide[V];
-    if (p.sigmoid) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const double t = exp_below(-__builtin_fabs((double)l[i])), r = one_over(1.0 + t);
-        wide[i] = l[i] < 0.f ? t * r : r;   // (of a NaN: NaN)
-      }
-    } else {
-      double total = 0.0;
-#pragma unroll
-      for (int i = 0; i < V; ++i) total += wide[i] = exp_below((double)l[i] - (double)most);
-      total = group_sum<LPT>(total);
-      sum = (float)total;
-      const double r = one_over(total);
-#pragma unroll
-      for (int i = 0; i < V; ++i) wide[i] *= r;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      key[i] = l[i] == -__builtin_inff() ? 0 : key_of(wide[i] + (double)p.bias[min(i * LPT + sub, p.E - 1)]);
-  } else {
-    if (!p.sigmoid) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) sum += expf(l[i] - most);
-      sum = group_sum<LPT>(sum);
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) key[i] = key_of(l[i]);
+    for (int i = 0; i < V; ++i) sum += e[i] = expf(l[i] - most);
+    sum = group_sum<LPT>(sum);
   }
   id = -1;
-  for (int j = 0; j < p.k; ++j) {
-    Key best = 0;
-    uint32_t at = 0;
+  if constexpr (!BIASED) {
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (key[i] > best) {   // (ascending experts: the first of equals stays)
-        best = key[i];
-        at = i * LPT + sub;
-      }
-    if constexpr (BIASED) {
-      fold_best<LPT>(best, at);
-    } else {
-      // one number: of equal keys the lower expert's is the larger
-      const uint64_t both = group_fold<LPT>((uint64_t)best << 32 | (uint32_t)~at, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-      best = (uint32_t)(both >> 32);
-      at = ~(uint32_t)both;
+    for (int i = 0; i < V; ++i) key[i] = key_of(l[i]);
+    choose_by_32<LPT>(key, p.k, sub, id, [](int, uint32_t) {});
+  } else {
+    // fp32 settles it where no two of the k + 1 largest come closer than twice their errors: a score's, below 2^-22 for the
+    // sigmoid and 2^-18 of the largest score for the softmax (rounded arguments, a sum of up to 1024), and one rounding of
+    // score + bias.  (One token in a hundred of 128 experts' random scores is not settled, so a workgroup of 64 most often
+    // has one; fp64 for all experts takes three times as long.)
+    const float scale = __builtin_amdgcn_rcpf(sum), apart = p.sigmoid ? 0x1p-20f : 0x1p-17f * scale;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float score = p.sigmoid ? __builtin_amdgcn_rcpf(1.f + expf(-l[i])) : e[i] * scale;
+      key[i] = l[i] == -__builtin_inff() ? 0 : key_of(score + p.bias[min(i * LPT + sub, p.E - 1)]);
     }
+    auto close = [&](uint32_t x, uint32_t y) {   // (NaN and infinities are)
+      const float a = value_of(x), b = value_of(y);
+      return x != 0 && y != 0 && !(a - b > apart + 0x1p-22f * fmaxf(fabsf(a), fabsf(b)));
+    };
+    bool inside = false, at_end = false;   // two of the first k are close; the last of them and the next
+    uint32_t before = 0;
+    choose_by_32<LPT>(key, p.k + 1, sub, id, [&](int j, uint32_t best) {
+      if (j < p.k) inside |= close(before, best);
+      else at_end = close(before, best);
+      before = best;
+    });
+    if (__ballot(inside || at_end)) {
+      double total = 0.0, r_total = 0.0;
+      if (!p.sigmoid) {
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i * LPT + sub == (int)at) key[i] = 0;
-    if (sub == j % LPT && best != 0) id = (int)at;
+        for (int i = 0; i < V; ++i) total += exp_below((double)l[i] - (double)most);
+        r_total = one_over(group_sum<LPT>(total));
+      }
+      auto exact = [&](float v, int at) {
+        double s;
+        if (p.sigmoid) {
+          const double t = exp_below(-__builtin_fabs((double)v)), r = one_over(1.0 + t);
+          s = v < 0.f ? t * r : r;   // (of a NaN: NaN)
+        } else {
+          s = exp_below((double)v - (double)most) * r_total;
+        }
+        return v == -__builtin_inff() ? 0 : key_of(s + (double)p.bias[at]);
+      };
+      // Which are the k or k + 1 first is settled in most of these too, only their order is not: it is a lane's own
+      // key among the others'.
+      int beyond_id = -1;
+      bool beyond = false;
+      choose_by_32<LPT>(key, 1, sub, beyond_id, [&](int, uint32_t best) { beyond = close(before, best); });
+      const int n = at_end ? p.k + 1 : p.k, base = (threadIdx.x & 63) - sub;
+      uint64_t own = 0;
+      if (id >= 0 && sub < n) own = exact(logit_at(p, token, id), id);
+      int rank = own != 0 ? 0 : sub;
+      for (int j = 0; j <= p.k; ++j) {
+        const uint64_t other = __shfl((unsigned long long)own, base + j);
+        const int there = __shfl(id, base + j);
+        if (own != 0 && j < n && j < LPT && (other > own || (other == own && there < id))) ++rank;
+      }
+      int sorted = id;
+      for (int j = 0; j <= p.k; ++j) {
+        const int to = __shfl(rank, base + j), there = __shfl(id, base + j);
+        if (j < LPT && to == sub) sorted = there;
+      }
+      id = sorted;
+      if (__ballot(at_end && (beyond || p.k == LPT))) {   // all of them by fp64 keys
+        uint64_t wide_key[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) wide_key[i] = exact(l[i], min(i * LPT + sub, p.E - 1));
+        id = -1;
+        choose_by_64<LPT>(wide_key, p.k, sub, id);
+      }
+    }
+    if (sub >= p.k) id = -1;
   }
   float score = 0.f;
   if (id >= 0) {

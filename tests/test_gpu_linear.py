@@ -425,6 +425,22 @@ def test_route_ties_masks_and_what_is_not_finite(fx, T, biased):
                                           None if bias is None else bias.astype(np.float64)))
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_route_of_scores_closer_than_32_bits_tell(fx, score):
+    """Biases that bring scores of different logits together up to a few times 2^-30: the 64-bit order decides."""
+    B, torch = fx
+    rng = np.random.default_rng(12)
+    T, E, k = 200, 96, 6
+    z = np.tile(rng.standard_normal(E), (T, 1)).astype(np.float32)
+    s = np.exp(z[0].astype(np.float64))
+    s = s / s.sum() if score == "softmax" else s / (1 + s)
+    # every biased score lies near 1 / 2, 3 / 4 or 1, as near as a float bias brings it
+    bias = (np.array([0.5, 0.75, 1.0])[rng.integers(0, 3, E)] - s).astype(np.float32)
+    z[100:, ::7] += (rng.standard_normal((100, len(z[0, ::7]))) * 2.0 ** -20).astype(np.float32)
+    plan = run_route(fx, torch.from_numpy(z).cuda(), k, score, True, 1.0, None, bias)
+    check_route(plan, route_reference(z.astype(np.float64), k, score, True, 1.0, None, bias.astype(np.float64)))
+
+
 def test_route_without_any_expert(fx):
     B, torch = fx
     for T in (3, 600):
