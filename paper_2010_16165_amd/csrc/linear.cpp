@@ -16,21 +16,21 @@ bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) !=
 constexpr int64_t kMostStride = int64_t(1) << 28;
 constexpr int64_t kMostElements = int64_t(1) << 44;
 
-fupr_status check_stride(int64_t stride, int64_t cols, int64_t rows, fupr_dtype dt) {
+fupr_status check_stride(int64_t stride, int64_t cols, int64_t rows, fupr_dtype dt, bool any = false) {
   if (stride < cols) return FUPR_ERR_SHAPE;
-  if (stride & (16 / bytes_of(dt) - 1)) return FUPR_ERR_ALIGN;
+  if (!any && (stride & (16 / bytes_of(dt) - 1))) return FUPR_ERR_ALIGN;
   if (stride > kMostStride || (rows > 0 && stride > kMostElements / rows)) return FUPR_ERR_LIMIT;
   return FUPR_OK;
 }
 
 }  // namespace
 
-fupr_status check_matrix(const fupr_matrix& m) {
+fupr_status check_matrix(const fupr_matrix& m, bool by_element) {
   if (!known_type(m.dt)) return FUPR_ERR_DTYPE;
   if (m.rows < 0 || m.cols < 1) return FUPR_ERR_SHAPE;
   if (m.rows > 0 && !m.ptr) return FUPR_ERR_NULL;
-  if (misaligned(m.ptr)) return FUPR_ERR_ALIGN;
-  return check_stride(m.stride, m.cols, m.rows, m.dt);
+  if (by_element ? (reinterpret_cast<uintptr_t>(m.ptr) & (bytes_of(m.dt) - 1)) != 0 : misaligned(m.ptr)) return FUPR_ERR_ALIGN;
+  return check_stride(m.stride, m.cols, m.rows, m.dt, by_element);
 }
 
 // Whether the two share an element's byte.  Matrices side by side in the rows of one buffer (one stride, other columns)

@@ -50,7 +50,7 @@ bool linear_rows_applies(const LinearParams& p);
 fupr_status launch_linear_rows(LinearParams p, fupr_dtype dt, void* stream);
 
 // linear.cpp: argument checks that the entry points share.
-fupr_status check_matrix(const fupr_matrix& m);
+fupr_status check_matrix(const fupr_matrix& m, bool by_element = false);   // by_element: any stride
 bool matrices_overlap(const fupr_matrix& a, const fupr_matrix& b);
 bool same_matrix(const fupr_matrix& a, const fupr_matrix& b);
 

@@ -516,7 +516,7 @@ fupr_status fupr_moe_route(const fupr_router* router, const fupr_matrix* logits,
                            void* stream) {
   if (!router || !logits || !offsets) return FUPR_ERR_NULL;
   fupr_status st = check_router(*router);
-  if (st != FUPR_OK || (st = check_matrix(*logits)) != FUPR_OK) return st;
+  if (st != FUPR_OK || (st = check_matrix(*logits, true)) != FUPR_OK) return st;
   if (logits->cols != router->E) return FUPR_ERR_SHAPE;
   if (logits->rows > 0 && (!ids || !weights || !src || !pos)) return FUPR_ERR_NULL;
   for (const void* v : {(const void*)ids, (const void*)weights, (const void*)offsets, (const void*)src, (const void*)pos})

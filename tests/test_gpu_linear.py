@@ -441,6 +441,21 @@ def test_route_of_scores_closer_than_32_bits_tell(fx, score):
     check_route(plan, route_reference(z.astype(np.float64), k, score, True, 1.0, None, bias.astype(np.float64)))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_route_of_logits_at_any_stride(fx, dtype):
+    """Contiguous rows of 60 or 7 experts, and columns in the middle of wider rows."""
+    B, torch = fx
+    rng = np.random.default_rng(60)
+    for T, E, k in ((1, 60, 8), (6, 60, 4), (333, 60, 8), (70, 7, 3)):
+        wide_rows = torch.from_numpy(rng.standard_normal((T, E + 5))).cuda().to(type_of(torch, dtype))
+        bias = (0.2 * rng.standard_normal(E)).astype(np.float32)
+        for logits in (wide_rows[:, :E].contiguous(), wide_rows[:, 3:E + 3]):
+            for b in (None, bias):
+                plan = run_route(fx, logits, k, "softmax", True, 1.0, None, b)
+                check_route(plan, route_reference(wide(logits), k, "softmax", True, 1.0, None,
+                                                  None if b is None else b.astype(np.float64)))
+
+
 def test_route_without_any_expert(fx):
     B, torch = fx
     for T in (3, 600):

@@ -108,6 +108,14 @@ def test_route_refuses():
         assert run(**{name: ADDR + 2}) == B.ERR_ALIGN
     assert run(bias=ADDR + 2) == B.ERR_ALIGN
     assert run(k=0) == run(k=9) == run(E=0) == run(cols=9) == B.ERR_SHAPE
+    router = B.RouterDesc(8, 2, 0, 1, 1.0, None, None)
+
+    def logits(dt, stride, ptr):
+        return B._lib.fupr_moe_route(C.byref(router), C.byref(mat(rows=0, cols=8, dt=dt, stride=stride, ptr=ptr)), ADDR, ADDR, ADDR,
+                                     ADDR, ADDR, None, 0, None)
+    assert logits(B.BF16, 9, ADDR + 2) == logits(B.F32, 11, ADDR + 4) == B.FUPR_OK   # rows of any stride
+    assert logits(B.BF16, 9, ADDR + 1) == logits(B.F32, 11, ADDR + 2) == B.ERR_ALIGN
+    assert logits(B.BF16, 7, ADDR) == B.ERR_SHAPE
     assert run(E=1025, cols=1025) == run(E=64, k=17, cols=64) == B.ERR_LIMIT
     assert run(T=(1 << 31) - 1, k=2) == B.ERR_LIMIT
     assert run(score=2) == run(renorm=2) == B.ERR_ARG
