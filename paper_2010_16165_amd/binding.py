@@ -628,12 +628,8 @@ class Router:
 
 
 def _stream(stream):
-    """The address of a stream handle; None: torch's current stream."""
-    if stream is not None:
-        return stream
-    if torch.cuda.is_initialized():
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
-    return torch.cuda.current_stream().cuda_stream
+    """The address of a stream handle; None: torch's current stream (a CUDA tensor is at hand, so torch has one)."""
+    return stream if stream is not None else torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def _ws(workspace):
@@ -677,14 +673,16 @@ def fupr_moe_route(router, logits, plan, stream=None):
 def fupr_moe_combine(y, pos, weights, res, out, stream=None):
     """out[t] = (res[t] +) sum_j weights[t, j] * y[pos[t, j]]; pos, weights: T x top_k."""
     where = "fupr_moe_combine"
-    if pos.dim() != 2 or weights.shape != pos.shape or pos.shape[0] != out.shape[0]:
+    shape = pos.shape
+    if len(shape) != 2 or weights.shape != shape or shape[0] != out.shape[0]:
         raise FuprError(ERR_SHAPE, where)
-    n = pos.numel()
+    n = shape[0] * shape[1]
     st = _lib.fupr_moe_combine(_matrix(y, where), _vector(pos, torch.int32, n, where),
-                               _vector(weights, torch.float32, n, where), pos.shape[1],
+                               _vector(weights, torch.float32, n, where), shape[1],
                                None if res is None else _matrix(res, where), _matrix(out, where),
                                _stream(stream))
-    _check(st, where)
+    if st:
+        _check(st, where)
 
 
 # ---- model ----------------------------------------------------------------------

@@ -4,9 +4,14 @@
 // asynchronous loads of 16 bytes per lane that need no registers, into a ring of D buffers.
 //
 // A wave multiplies unit u from registers while it reads unit u + 1 from LDS into them.  One barrier for U units: behind
-// it the next U may be read, and the buffers of the last U are asked for again, one unit's loads at a time.  The loads are spread between the multiplications - a wave that finds
-// the load queue full cannot issue what stands behind.  A filter's operand registers are refilled as soon as its
-// last multiplication is issued; only the operands of the last rows and the filters exist twice.
+// it the next U may be read, and the buffers of the last U are asked for again, one unit's loads at a time.  The loads
+// are spread between the multiplications - a wave that finds the load queue full cannot issue what stands behind.  A
+// filter's operand registers are refilled as soon as its last multiplication is issued; only the operands of the last
+// rows and the filters exist twice.
+//
+// Where there are few tiles a unit's latency bounds them, so KS groups of waves share a tile's reduction: group g takes
+// units g, g + KS, ..., each group in a ring of its own, and the sums meet in LDS in the groups' order (256 x 1000 x 2048
+// in fp32: 40 us in tiles of 64 x 64 without groups, 16 us in tiles of 32 x 32 with four).
 //
 // LDS row r (64 bytes) holds its four chunks at chunk ^ (r / 2 & 3).  LDS serves 16 lanes of an operand read at a time
 // (four times four neighbours, not of one chunk): with this order they cover all 64 banks once, 233 bytes per clock
