@@ -52,6 +52,30 @@ __device__ __forceinline__ float logit_at(const RouteParams& p, int64_t token, i
   return p.dt == FUPR_BF16 ? to_float<true>(h) : to_float<false>(h);
 }
 
+// The logits of experts sub, sub + LPT, ...; -inf of those that do not exist.
+template <int LPT, int V>
+__device__ __forceinline__ void load_logits(const RouteParams& p, int64_t token, int sub, float (&l)[V]) {
+  const char* row = p.logits + token * p.stride;
+  if (p.dt == FUPR_F32) {
+    const float* r = reinterpret_cast<const float*>(row) + sub;
+#pragma unroll
+    for (int i = 0; i < V; ++i) l[i] = i * LPT + sub < p.E ? r[i * LPT] : -__builtin_inff();
+  } else {
+    const uint16_t* r = reinterpret_cast<const uint16_t*>(row) + sub;
+    const bool bf = p.dt == FUPR_BF16;
+    uint16_t h[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = i * LPT + sub < p.E ? r[i * LPT] : bf ? 0xff80 : 0xfc00;
+#pragma unroll
+    for (int i = 0; i < V; ++i) l[i] = bf ? to_float<true>(h[i]) : to_float<false>(h[i]);
+  }
+  if (p.keep) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i * LPT + sub < p.E && p.keep[i * LPT + sub] == 0) l[i] = -__builtin_inff();
+  }
+}
+
 // Keys as unsigned numbers in the same order; 0: not to be chosen (-inf), all ones: NaN.
 __device__ __forceinline__ uint32_t key_of(float v) {
   if (v != v) return ~0u;
@@ -123,20 +147,16 @@ __device__ __forceinline__ float value_of(uint32_t key) {   // of which key_of m
 template <int LPT, int V, class Each>
 __device__ __forceinline__ void choose_by_32(uint32_t (&key)[V], int rounds, int sub, int& id, Each each) {
   for (int j = 0; j < rounds; ++j) {
-    uint32_t best = 0, at = 0;
+    uint32_t best = key[0];
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (key[i] > best) {   // (ascending experts: the first of equals stays)
-        best = key[i];
-        at = i * LPT + sub;
-      }
-    // one number: of equal keys the lower expert's is the larger
-    const uint64_t both = group_fold<LPT>((uint64_t)best << 32 | (uint32_t)~at, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-    best = (uint32_t)(both >> 32);
-    at = ~(uint32_t)both;
+    for (int i = 1; i < V; ++i) best = max(best, key[i]);
+    best = group_fold<LPT>(best, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+    uint32_t at = ~0u;
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i * LPT + sub == (int)at) key[i] = 0;
+    for (int i = V; i-- > 0;) at = key[i] == best ? (uint32_t)(i * LPT) : at;   // (of equals the first)
+    at = group_fold<LPT>(at == ~0u ? at : at + sub, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+#pragma unroll
+    for (int i = 0; i < V; ++i) key[i] = at == (uint32_t)(i * LPT + sub) ? 0 : key[i];
     if (sub == j && best != 0) id = (int)at;
     each(j, best);
   }
@@ -166,11 +186,7 @@ template <int LPT, int V, bool BIASED>
 __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int sub, int& id, float& weight) {
   float l[V], e[V];
   uint32_t key[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int at = i * LPT + sub;
-    l[i] = at < p.E && !(p.keep && p.keep[at] == 0) ? logit_at(p, token, at) : -__builtin_inff();
-  }
+  load_logits<LPT>(p, token, sub, l);
   // softmax: the largest logit and the sum of exponentials (an expert that does not exist has e^-inf = 0)
   float most = -__builtin_inff(), sum = 0.f;
   if (!p.sigmoid) {
@@ -192,11 +208,14 @@ __device__ __forceinline__ void choose(const RouteParams& p, int64_t token, int 
     // sigmoid and 2^-18 of the largest score for the softmax (rounded arguments, a sum of up to 1024), and one rounding of
     // score + bias.  (One token in a hundred of 128 experts' random scores is not settled, so a workgroup of 64 most often
     // has one; fp64 for all experts takes three times as long.)
+    float bias[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) bias[i] = i * LPT + sub < p.E ? p.bias[i * LPT + sub] : 0.f;
     const float scale = __builtin_amdgcn_rcpf(sum), apart = p.sigmoid ? 0x1p-20f : 0x1p-17f * scale;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float score = p.sigmoid ? __builtin_amdgcn_rcpf(1.f + expf(-l[i])) : e[i] * scale;
-      key[i] = l[i] == -__builtin_inff() ? 0 : key_of(score + p.bias[min(i * LPT + sub, p.E - 1)]);
+      key[i] = l[i] == -__builtin_inff() ? 0 : key_of(score + bias[i]);
     }
     auto close = [&](uint32_t x, uint32_t y) {   // (NaN and infinities are)
       const float a = value_of(x), b = value_of(y);
