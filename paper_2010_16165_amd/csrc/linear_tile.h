@@ -76,13 +76,13 @@ __device__ __forceinline__ Addend<TY> load_addend(const LinearParams& p, int64_t
   }
   return a;
 }
-template <int TY>
+template <int TY, bool RES>
 __device__ __forceinline__ void store_row(const LinearParams& p, int64_t row, int n, float (&v)[8], const Addend<TY>& add) {
   const bool whole = n + 8 <= p.N;
   const uint32_t d[8] = {add.v[0].x, add.v[0].y, add.v[0].z, add.v[0].w, add.v[1].x, add.v[1].y, add.v[1].z, add.v[1].w};
   if (TY == FUPR_F32 || p.y_f32) {
     float* y = reinterpret_cast<float*>(p.y + row * p.y_stride) + n;
-    if (p.res) {
+    if constexpr (RES) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(d[i]);
     }
@@ -97,7 +97,7 @@ __device__ __forceinline__ void store_row(const LinearParams& p, int64_t row, in
   } else {
     constexpr bool BF = TY == FUPR_BF16;
     uint16_t* y = reinterpret_cast<uint16_t*>(p.y + row * p.y_stride) + n;
-    if (p.res) {
+    if constexpr (RES) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += to_float<BF>((uint16_t)(d[i / 2] >> (i & 1) * 16));
     }
@@ -145,18 +145,19 @@ __device__ __forceinline__ FinishInputs<TY> ask_finish(const LinearParams& p, bo
 }
 // Rows of NT * 4 chunks of four columns (gated: the gate's half, then the other's), chunk c at c ^ (row modulo chunks), in
 // KS copies `apart` bytes from each other, whose sum is the result.
-template <int TY, int NT, int KS, bool GATED>
-__device__ __forceinline__ void finish_rows(const LinearParams& p, FinishInputs<TY> in, const char* lds, int apart, int from_row,
+//
+// Loads and stores retire in order, so a load that is waited for waits for the stores before it: without a residual the
+// loop has no load at all, with one the two addends under way stay in registers of their own (a move would wait).  Waiting
+// for every store cost a tile of 256 x 256 some 5 us.
+template <int TY, int NT, int KS, bool GATED, bool RES>
+__device__ __forceinline__ void finish_loop(const LinearParams& p, FinishInputs<TY>& in, const char* lds, int apart, int from_row,
                                             int rows, int hi, int first, int nb, int n_len, int lane) {
   constexpr bool FINE = TY == FUPR_F32;
   constexpr int CHUNKS = NT * 4, kLanes = finish_lanes<NT>(GATED), kTurn = 64 / kLanes;
   const int c = lane % kLanes, n = nb + c * 8;
-#pragma unroll 1
-  for (int r = from_row + lane / kLanes; r < rows; r += kTurn) {
+  auto turn = [&](int r, Addend<TY>& add) {
+    if (r >= rows) return;
     const int row = first + r, later = r + 2 * kTurn;
-    const Addend<TY> add = in.next;
-    in.next = in.after;
-    in.after = load_addend<TY>(p, first + later, n, later < rows && first + later < hi);
     const char* from = lds + r * CHUNKS * 16;
     float v[8], u[8];
 #pragma unroll
@@ -184,8 +185,20 @@ __device__ __forceinline__ void finish_rows(const LinearParams& p, FinishInputs<
       if constexpr (GATED) v[i] *= u[i];
       if (n + i >= n_len) v[i] = 0.f;   // columns that pruning took from this expert
     }
-    if (row < hi && n < p.N) store_row<TY>(p, row, n, v, add);
+    if (row < hi && n < p.N) store_row<TY, RES>(p, row, n, v, add);
+    if constexpr (RES) add = load_addend<TY>(p, first + later, n, later < rows && first + later < hi);
+  };
+#pragma unroll 1
+  for (int r = from_row + lane / kLanes; r < rows; r += RES ? 2 * kTurn : kTurn) {
+    turn(r, in.next);
+    if constexpr (RES) turn(r + kTurn, in.after);
   }
+}
+template <int TY, int NT, int KS, bool GATED>
+__device__ __forceinline__ void finish_rows(const LinearParams& p, FinishInputs<TY>& in, const char* lds, int apart, int from_row,
+                                            int rows, int hi, int first, int nb, int n_len, int lane) {
+  if (p.res) finish_loop<TY, NT, KS, GATED, true>(p, in, lds, apart, from_row, rows, hi, first, nb, n_len, lane);
+  else finish_loop<TY, NT, KS, GATED, false>(p, in, lds, apart, from_row, rows, hi, first, nb, n_len, lane);
 }
 
 // A wave's accumulators of EM x NT tiles of 16 x 16 to LDS, as finish_rows reads them.
@@ -207,10 +220,12 @@ template <int TY, int MT, int NT, int EM, bool GATED>
 __device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4 (&acc)[MT][NT], char* lds, int e, int hi,
                                               int row0, int nb, int n_len, int lane) {
   static_assert(MT % EM == 0, "whole parts");
+  // (written out: accumulators chosen in a loop would live in memory)
 #pragma unroll
   for (int part = 0; part < MT / EM; ++part) {
     const int first = row0 + part * EM * 16;
-    const FinishInputs<TY> in = ask_finish<TY, NT>(p, GATED, 0, EM * 16, e, hi, first, nb, n_len, lane);
+    if (first >= hi) break;
+    FinishInputs<TY> in = ask_finish<TY, NT>(p, GATED, 0, EM * 16, e, hi, first, nb, n_len, lane);
     stage_tiles<MT, NT, EM, GATED>(acc, part * EM, lds, lane);
     finish_rows<TY, NT, 1, GATED>(p, in, lds, 0, 0, EM * 16, hi, first, nb, n_len, lane);
   }
@@ -218,7 +233,7 @@ __device__ __forceinline__ void tile_epilogue(const LinearParams& p, const f32x4
 
 // The same of tiles whose reduction KS groups of waves share, `apart` bytes of LDS each: a group finishes a part of the rows.
 template <int TY, int MT, int NT, int KS, bool GATED>
-__device__ __forceinline__ void shared_epilogue(const LinearParams& p, const FinishInputs<TY>& in, const f32x4 (&acc)[MT][NT], char* lds,
+__device__ __forceinline__ void shared_epilogue(const LinearParams& p, FinishInputs<TY>& in, const f32x4 (&acc)[MT][NT], char* lds,
                                                 int apart, int group, int hi, int row0, int nb, int n_len, int lane) {
   constexpr int kRows = MT * 16 / KS;
   static_assert(MT * 16 % KS == 0, "whole rows");
