@@ -92,11 +92,11 @@ constexpr TileCost kCosts[kLinearTiles] = {
     {16, 16, 1, 0.6f, 1.0f, 0.050f, 0.050f, 0.050f, 0.050f},
     {32, 32, 1, 0.6f, 2.6f, 0.045f, 0.060f, 0.085f, 0.095f},
     {32, 64, 2, 0.6f, 2.4f, 0.070f, 0.145f, 0.14f, 0.26f},
-    {64, 64, 2, 0.6f, 2.8f, 0.118f, 0.25f, 0.27f, 0.52f},
-    {64, 128, 2, 0.6f, 4.0f, 0.19f, 0.48f, 0.48f, 0.92f},
-    {128, 128, 2, 0.6f, 4.8f, 0.32f, 0.62f, 0.93f, 1.9f},
-    {128, 256, 1, 0.6f, 6.0f, 0.29f, 0.42f, 0.f, 0.f},
-    {256, 256, 1, 0.4f, 8.7f, 0.54f, 0.72f, 0.f, 0.f},
+    {64, 64, 2, 0.6f, 2.5f, 0.118f, 0.25f, 0.27f, 0.52f},
+    {64, 128, 2, 0.6f, 3.1f, 0.19f, 0.48f, 0.48f, 0.92f},
+    {128, 128, 2, 0.6f, 3.2f, 0.32f, 0.62f, 0.93f, 1.9f},
+    {128, 256, 1, 0.6f, 4.6f, 0.29f, 0.42f, 0.f, 0.f},
+    {256, 256, 1, 0.4f, 6.2f, 0.54f, 0.72f, 0.f, 0.f},
 };
 
 // The kernel whose tiles are through first: small ones put more compute units to work, large ones read less for
