@@ -90,9 +90,9 @@ struct TileCost {
 };
 constexpr TileCost kCosts[kLinearTiles] = {
     {16, 16, 1, 0.6f, 1.0f, 0.050f, 0.050f, 0.050f, 0.050f},
-    {32, 32, 1, 0.6f, 2.6f, 0.045f, 0.060f, 0.085f, 0.095f},
-    {32, 64, 2, 0.6f, 2.4f, 0.070f, 0.145f, 0.14f, 0.26f},
-    {64, 64, 2, 0.6f, 2.5f, 0.118f, 0.25f, 0.27f, 0.52f},
+    {32, 32, 1, 0.6f, 2.1f, 0.042f, 0.060f, 0.085f, 0.095f},
+    {32, 64, 2, 0.6f, 2.1f, 0.070f, 0.145f, 0.14f, 0.26f},
+    {64, 64, 2, 0.6f, 2.2f, 0.118f, 0.25f, 0.27f, 0.52f},
     {64, 128, 2, 0.6f, 3.1f, 0.19f, 0.48f, 0.48f, 0.92f},
     {128, 128, 2, 0.6f, 3.2f, 0.32f, 0.62f, 0.93f, 1.9f},
     {128, 256, 1, 0.6f, 4.6f, 0.29f, 0.42f, 0.f, 0.f},
@@ -131,7 +131,7 @@ LinearTile choose_tile(const LinearParams& p, fupr_dtype dt) {
     // (where compute units take two, those that do set the pace; where one, it is the load on memory and power)
     const float more = rest <= 0.5f ? 0.f : c.at_once > 1 ? 1.f : 2.f * rest - 1.f;
     float cost = full * (begin + units * hi) + (rest > 0.f ? begin + units * (lo + (hi - lo) * more) : 0.f);
-    if (t == kRows16x16) cost = (fill > 1.f ? fill : 1.f) * (begin + units * lo);   // (many at a time: no rounds)
+    if (t == kRows16x16) cost = (fill > 1.f ? 1.15f * fill : 1.f) * (begin + units * lo);   // (many at a time: no rounds)
     if (which < 0 || cost < best) {
       best = cost;
       which = t;

@@ -173,6 +173,22 @@ __device__ __forceinline__ int tile_of_workgroup(int id, int total) {
   return (id >> 3) < each && at < total ? at : -1;
 }
 
+// COUNT biases from element `at` on, the first `there` of which exist; no vector: zeros.
+template <int COUNT>
+__device__ __forceinline__ void load_biases(const float* from, int64_t at, int there, float (&to)[COUNT]) {
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i) to[i] = 0.f;
+  if (!from) return;
+  if (there >= COUNT) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) to[i] = from[at + i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+      if (i < there) to[i] = from[at + i];
+  }
+}
+
 // What is added to four consecutive results of one row from column n on, in its own type (16 bits: in two words).  Whole
 // pieces are read, also of a row that ends inside one: a row's memory extends to its stride.
 template <int TY>

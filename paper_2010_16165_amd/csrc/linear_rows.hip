@@ -63,15 +63,11 @@ __global__ __launch_bounds__(kWaves * 64) void linear_rows_kernel(LinearParams p
   // what the epilogue adds, on its way before the weights are: 0.6 us less at the end of a launch of 5 us
   const int n = n0 + g * 4;
   const bool finishes = wave == 0 && row < hi;
-  f32x4 bias = zero, bias_up = zero;
+  float bias[4] = {}, bias_up[4] = {};
   uint4 add = {0u, 0u, 0u, 0u};
   if (finishes) {
-    const int64_t bias_at = (int64_t)e * p.N + n;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (p.bias && n + i < n_len) bias[i] = p.bias[bias_at + i];
-      if (GATED && p.bias_up && n + i < n_len) bias_up[i] = p.bias_up[bias_at + i];
-    }
+    load_biases<4>(p.bias, (int64_t)e * p.N + n, n_len - n, bias);
+    if constexpr (GATED) load_biases<4>(p.bias_up, (int64_t)e * p.N + n, n_len - n, bias_up);
     add = load_four<TY>(p, row, n);
   }
 
@@ -129,7 +125,7 @@ __global__ __launch_bounds__(kWaves * 64) void linear_rows_kernel(LinearParams p
   __syncthreads();
   if (!finishes) return;
   constexpr bool FINE = TY == FUPR_F32;
-  f32x4 v = bias, up = bias_up;
+  f32x4 v = {bias[0], bias[1], bias[2], bias[3]}, up = {bias_up[0], bias_up[1], bias_up[2], bias_up[3]};
 #pragma unroll
   for (int k = 0; k < kWaves; ++k) {
     v += part[k][0][lane];

@@ -133,11 +133,8 @@ __device__ __forceinline__ FinishInputs<TY> ask_finish(const LinearParams& p, bo
   const int lanes = finish_lanes<NT>(gated), turn = 64 / lanes;
   const int n = nb + lane % lanes * 8;
   FinishInputs<TY> in;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    in.bias[i] = p.bias && n + i < n_len ? p.bias[(int64_t)e * p.N + n + i] : 0.f;
-    in.up[i] = p.bias_up && n + i < n_len ? p.bias_up[(int64_t)e * p.N + n + i] : 0.f;
-  }
+  load_biases<8>(p.bias, (int64_t)e * p.N + n, n_len - n, in.bias);
+  load_biases<8>(p.bias_up, (int64_t)e * p.N + n, n_len - n, in.up);
   const int r = from_row + lane / lanes;
   in.next = load_addend<TY>(p, first + r, n, r < rows && first + r < hi);
   in.after = load_addend<TY>(p, first + r + turn, n, r + turn < rows && first + r + turn < hi);

@@ -79,11 +79,6 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
 
   const int wm = wave / G::WN, wn = wave % G::WN;
   const int row0 = m0 + wm * MT * 16, nb = n0 + wn * NT * (gated ? 8 : 16);
-  // small tiles have registers to ask for what the epilogue adds before they begin
-  constexpr bool kEarly = MT * NT <= 4;
-  FinishInputs<G::TY> in;
-  if constexpr (kEarly)
-    in = ask_finish<G::TY, NT>(p, gated, group * (MT * 16 / KS), (group + 1) * (MT * 16 / KS), e, hi, row0, nb, n_len, lane);
 
   // One load of unit `issued`, into buffer `to`.  In the unit that the reduction ends in, chunks behind its last one are
   // that last one again (inside the row, and zeroed below).
@@ -173,15 +168,21 @@ __global__ __launch_bounds__(G::threads, 2) void linear_tile_kernel(LinearParams
     if (more) end_unit();
   };
 
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+    if (issued < units) {
+      begin_unit();
+#pragma unroll
+      for (int i = 0; i < G::loads; ++i) load(i);
+      end_unit();
+    }
+  // small tiles have registers to ask for what the epilogue adds before their first multiplication
+  constexpr bool kEarly = MT * NT <= 4;
+  FinishInputs<G::TY> in;
+  if constexpr (kEarly)
+    in = ask_finish<G::TY, NT>(p, gated, group * (MT * 16 / KS), (group + 1) * (MT * 16 / KS), e, hi, row0, nb, n_len, lane);
   if (units > 0) {
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-      if (issued < units) {
-        begin_unit();
-#pragma unroll
-        for (int i = 0; i < G::loads; ++i) load(i);
-        end_unit();
-      }
+    // (of all loads under way: those of the epilogue make this wait a little longer than it has to)
     if (units >= D) wait_loads<(D - U) * G::loads>();
     else wait_loads<0>();
     if (ragged && units <= U) clear_tail((units - 1) * G::buf);
